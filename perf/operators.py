@@ -1,0 +1,614 @@
+"""What a streaming video model asks of this library around its attention calls, as timed cases.
+
+A model that generates a video chunk after chunk normalises and rotates the queries and keys of a chunk, writes its
+keys and values into a cache in 8 bits, and attends from the chunk's queries to all the cache holds.  A case is one such
+call, a dict of plain values:
+
+  op        "norm"      asa_qk_norm_rope: norm of queries and keys for each head, and their rotation by position
+            "norm_bwd"  asa_qk_norm_rope_bwd: its gradients
+            "cache"     asa_cache_write of new tokens behind those held, asa_cache_read of the blocks they went to
+            "attn"      asa_attn_cache
+  B, H, Hkv, d          batch, query heads, key heads, head size
+  L                     tokens of the call (queries of "attn")
+  packed                q and k (k and v) are slices of one projection [B, L, heads * d]
+
+norm:   kind "rms" | "layer"; pairing "adjacent" | "halves"; rot rotated channels; T, Y, X the grid whose positions
+        the tables hold; first table row of token 0 (negative: text in front, which is not rotated); ragged: every
+        sequence starts at a row of its own
+cache:  block, held (tokens in the cache before the call, at most), blocks (capacity)
+attn:   block, held (tokens in the cache, at most; ragged: less in some sequences), kept (share of the blocks in
+        the lists; 1: no lists)
+"""
+
+import math
+
+import torch
+
+own = False
+DEV = "cuda"
+EPS = 1e-6
+LARGEST = 448.0              # of the 8-bit type, e4m3: 4 significant bits
+LEAST_EXP, MOST_EXP = -100, 120
+
+
+def _norm(name, op, B, H, Hkv, L, d, kind, pairing, rot, grid, first=0, packed=True, ragged=False):
+    return {"name": name, "op": op, "B": B, "H": H, "Hkv": Hkv, "L": L, "d": d, "kind": kind, "pairing": pairing, "rot": rot,
+            "T": grid[0], "Y": grid[1], "X": grid[2], "first": first, "packed": packed, "ragged": ragged}
+
+
+def _cache(name, B, Hkv, L, d, block, held, blocks, packed=True):
+    return {"name": name, "op": "cache", "B": B, "Hkv": Hkv, "L": L, "d": d, "block": block, "held": held, "blocks": blocks,
+            "packed": packed}
+
+
+def _attn(name, B, H, Hkv, L, d, block, held, kept=1.0, ragged=False, packed=False):
+    return {"name": name, "op": "attn", "B": B, "H": H, "Hkv": Hkv, "L": L, "d": d, "block": block, "held": held, "kept": kept,
+            "ragged": ragged, "packed": packed}
+
+
+_WAN = (21, 30, 52)      # Wan2.1-1.3B: 32 760 video tokens, 12 heads of 128
+_COG = (13, 30, 45)      # CogVideoX-5B: 17 550 video tokens behind 226 text tokens, 48 heads of 64
+
+
+def listed():
+    return [
+        # One token for each of eight sequences: what a token-by-token model calls in every layer.  A launch decides.
+        _norm("norm_token", "norm", 8, 12, 12, 1, 128, "rms", "halves", 128, (1, 1, 8192), ragged=True),
+        # A whole video at the Wan shape, straight out of the projection.
+        _norm("norm_wan", "norm", 1, 12, 12, 32760, 128, "rms", "adjacent", 128, _WAN),
+        # CogVideoX: mean and variance, weights and biases, text tokens in front that are not rotated.
+        _norm("norm_cog", "norm", 1, 48, 48, 17776, 64, "layer", "adjacent", 64, _COG, first=-226),
+        # Training at the Wan shape.
+        _norm("norm_wan_bwd", "norm_bwd", 1, 12, 12, 32760, 128, "rms", "adjacent", 128, _WAN),
+        # Training at a medium size nothing divides: shared key heads, half the channels rotated, in halves.
+        _norm("norm_mid_bwd", "norm_bwd", 2, 10, 5, 4332, 64, "layer", "halves", 32, (5, 23, 37), first=-77, packed=False),
+        # One token more for each of sixteen sequences, into blocks that hold some.
+        _cache("cache_token", 16, 8, 1, 128, 128, 4000, 64),
+        # Three latent frames (4 680 tokens) of the Wan shape behind six, which end inside a block.
+        _cache("cache_chunk", 1, 12, 4680, 128, 128, 9360, 256),
+        # Two whole videos of many small heads at once: a prompt video, before anything is generated.
+        _cache("cache_video", 2, 48, 17776, 64, 64, 0, 280, packed=False),
+        # One token for each of sixteen sequences, four query heads on a key head, all lengths up to 8 000.
+        _attn("attn_token", 16, 32, 8, 1, 128, 128, 8000, ragged=True),
+        # One token on a single very long sequence: few rows, all of the chip on one axis.
+        _attn("attn_token_long", 1, 12, 12, 1, 128, 128, 131000),
+        # A chunk of three latent frames on the cache of a whole Wan video, every block.
+        _attn("attn_chunk", 1, 12, 12, 4680, 128, 128, 32760, packed=True),
+        # A latent frame of many small heads with a quarter of the blocks: small blocks, lists, a ragged end.
+        _attn("attn_chunk_sparse", 1, 48, 48, 1350, 64, 64, 17776, kept=0.25),
+    ]
+
+
+def _log_between(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.49)))))))
+
+
+def draw(rng):
+    op = rng.choice(["norm", "norm", "norm_bwd", "norm_bwd", "cache", "cache", "attn", "attn", "attn"])
+    d, block = rng.choice([64, 128]), rng.choice([64, 128])
+    Hkv, group = _log_between(rng, 1, 48), rng.choice([1, 1, 1, 2, 3, 4, 8])
+    if op in ("norm", "norm_bwd"):
+        H = min(48, Hkv * group)
+        Hkv = H // group if H % group == 0 and H >= group else H
+        most = 24 * 32760 * 128                           # elements of q and k in the largest listed call
+        L = _log_between(rng, 1 if op == "norm" else 60, 32760)
+        L = max(1, min(L, most // ((H + Hkv) * d)))
+        B = rng.randint(1, max(1, min(8, most // ((H + Hkv) * d * L))))
+        T = rng.randint(1, max(1, min(21, L // 60)))
+        X = max(1, round(math.sqrt(L / T / rng.uniform(0.45, 1.0))))
+        Y = max(1, -(-L // (T * X)))
+        text = rng.choice([0, 0, rng.randint(1, 300)])
+        return _norm("", op, B, H, Hkv, L, d, rng.choice(["rms", "layer"]), rng.choice(["adjacent", "halves"]),
+                     rng.choice([d, d, d // 2, 16]), (T, Y, X), first=-min(text, L - 1), packed=rng.random() < 0.6,
+                     ragged=rng.random() < 0.3) | {"name": "drawn"}
+    if op == "cache":
+        L = rng.choice([1, rng.randint(2, 200), _log_between(rng, 200, 32760), _log_between(rng, 200, 32760)])
+        L = min(L, 2 * 48 * 17776 * 64 // (Hkv * d))
+        B = rng.randint(1, max(1, min(16, 2 * 48 * 17776 * 64 // (Hkv * d * L))))
+        held = rng.choice([0, rng.randint(1, 20000)])
+        held = min(held, 6 * 48 * 17776 * 64 // (Hkv * d * B))
+        return _cache("drawn", B, Hkv, L, d, block, held, (held + L + block - 1) // block + 2, packed=rng.random() < 0.5)
+    H = Hkv * group if Hkv * group <= 64 else Hkv
+    L = rng.choice([1, 1, rng.randint(2, 100), _log_between(rng, 100, 4680), _log_between(rng, 100, 4680)])
+    held = _log_between(rng, 1, 131000)
+    scores = 4680 * 32760 * 12
+    held = max(1, min(held, scores // (H * L), 131000 * 12 * 128 // (Hkv * d)))
+    B = rng.randint(1, max(1, min(16, scores // (H * L * held), 131000 * 12 * 128 // (Hkv * d * held))))
+    kept = rng.choice([1.0, 1.0, round(rng.uniform(0.1, 0.7), 2)])
+    return _attn("drawn", B, H, Hkv, L, d, block, held, kept=kept, ragged=rng.random() < 0.5, packed=rng.random() < 0.5)
+
+
+# ------------------------------------------------------------------------------------------ the 8-bit cache
+#
+# K [B, Hkv, blocks, block / 32, d / 16, 32 tokens, 16 channels]: groups of 32 tokens, in pieces of 16 channels.
+# V [B, Hkv, blocks, block / 32, d / 32, 2, 32 channels, 16 tokens]: byte 4 m + j of half h is token 8 m + 4 h + j.
+
+def _k_codes(codes):
+    """[.., tokens, d] -> the layout of K, tokens a multiple of 32."""
+    *lead, n, d = codes.shape
+    return codes.reshape(*lead, n // 32, 32, d // 16, 16).transpose(-3, -2)
+
+
+def _k_tokens(stored):
+    """The layout of K [.., groups, d / 16, 32, 16] -> [.., tokens, d]."""
+    *lead, g, c, _, _ = stored.shape
+    return stored.transpose(-3, -2).reshape(*lead, g * 32, c * 16)
+
+
+def _v_codes(codes):
+    *lead, n, d = codes.shape
+    x = codes.reshape(*lead, n // 32, 4, 2, 4, d // 32, 32)          # group, m, h, j, channel tile, channel
+    k = len(lead)
+    return x.permute(*range(k), k, k + 4, k + 2, k + 5, k + 1, k + 3).reshape(*lead, n // 32, d // 32, 2, 32, 16)
+
+
+def _v_tokens(stored):
+    *lead, g, c, _, _, _ = stored.shape
+    x = stored.reshape(*lead, g, c, 2, 32, 4, 4)                     # group, channel tile, h, channel, m, j
+    k = len(lead)
+    return x.permute(*range(k), k, k + 4, k + 2, k + 5, k + 1, k + 3).reshape(*lead, g * 32, c * 32)
+
+
+def _power(e):
+    """2^e in 64 bits from its bits, -1022 <= e <= 1023 (a power function may miss by a last bit)."""
+    return ((e.to(torch.int64) + 1023) << 52).view(torch.float64)
+
+
+def _scale_for(absmax):
+    """The least power of two 2^e, LEAST_EXP <= e <= MOST_EXP, with absmax <= 448 * 2^e (absmax < 2^128)."""
+    m, x = torch.frexp(absmax)                                       # absmax = m 2^x, 1/2 <= m < 1; 448 = 7/8 2^9
+    e = torch.where(m > 0.875, x - 8, x - 9)
+    e = torch.where(absmax == 0, torch.full_like(e, LEAST_EXP), e).clamp(LEAST_EXP, MOST_EXP)
+    return _power(e).float()
+
+
+def _absmax(x, dims, among=None):
+    a = torch.where(torch.isfinite(x), x, torch.zeros((), device=x.device)).abs()
+    if among is not None:
+        a = torch.where(among, a, torch.zeros((), device=x.device))
+    return a.amax(dims)
+
+
+def _value(code):
+    return code.view(torch.float8_e4m3fn).float()
+
+
+def _encode(x):
+    """fp32 values of at most 448 -> codes; what is not finite becomes the type's NaN."""
+    x = torch.where(torch.isfinite(x), x, torch.full((), float("nan"), device=x.device))
+    return x.to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+def _new_cache(k, v, block, blocks):
+    """The cache of k, v [B, Hkv, n, d] fp32, written at once; n at most blocks * block."""
+    B, Hkv, n, d = k.shape
+    out = []
+    for x, lay in ((k, _k_codes), (v, _v_codes)):
+        full = torch.zeros(B, Hkv, blocks * block, d, device=DEV)
+        full[:, :, :n] = x
+        full = full.reshape(B, Hkv, blocks, block, d)
+        scale = _scale_for(_absmax(full, (-2, -1)))
+        out += [lay(_encode(full / scale[..., None, None])).contiguous(), scale]
+        del full
+    return {"kc": out[0], "ks": out[1], "vc": out[2], "vs": out[3]}
+
+
+# ------------------------------------------------------------------------------------------ inputs
+
+def _tables(c):
+    """cos and sin [T Y X, rot / 2]: the channels' pairs are shared out among the three axes of the video grid."""
+    pairs = c["rot"] // 2
+    n = [pairs - 2 * (pairs // 3), pairs // 3, pairs // 3]
+    pos = torch.meshgrid(*(torch.arange(c[a], dtype=torch.float64, device=DEV) for a in "TYX"), indexing="ij")
+    parts = [p.reshape(-1, 1) * 10000.0 ** (-torch.arange(m, dtype=torch.float64, device=DEV) / max(m, 1)) for p, m in zip(pos, n)]
+    angle = torch.cat(parts, dim=1)
+    return angle.cos().float().contiguous(), angle.sin().float().contiguous()
+
+
+def _heads(packed, g, B, counts, L, d, gain):
+    """One tensor [B, n, L, d] bf16 for each n of `counts`; views of one projection [B, L, sum * d] where packed."""
+    x = torch.randn(B, L, sum(counts), d, device=DEV, generator=g) * gain
+    if packed:
+        x = x.to(torch.bfloat16)
+        return [p.transpose(1, 2) for p in x.split(counts, dim=2)]
+    return [p.transpose(1, 2).contiguous().to(torch.bfloat16) for p in x.split(counts, dim=2)]
+
+
+def _like(x):
+    """A tensor of zeros with x's sizes and strides (heads next to each other in memory where x has them so)."""
+    if x.is_contiguous():
+        return torch.zeros_like(x)
+    B, n, L, d = x.shape
+    return torch.zeros(B, L, n, d, device=DEV, dtype=x.dtype).transpose(1, 2)
+
+
+def prepare(case, seed):
+    c = case
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    B, L, d = c["B"], c["L"], c["d"]
+    s = {"c": c}
+    if c["op"] in ("norm", "norm_bwd"):
+        H, Hkv = c["H"], c["Hkv"]
+        gain = torch.exp(0.5 * torch.randn(H + 2 * Hkv, d, device=DEV, generator=g))
+        q, k, _ = _heads(c["packed"], g, B, [H, Hkv, Hkv], L, d, gain)
+        cos, sin = _tables(c)
+        s.update(q=q, k=k, cos=cos, sin=sin, start=None)
+        if c["ragged"]:
+            s["start"] = torch.randint(0, max(1, cos.shape[0] - L + 1), (B,), device=DEV, generator=g, dtype=torch.int32)
+        for x in "qk":
+            s[x + "w"] = 1.0 + 0.3 * torch.randn(d, device=DEV, generator=g)
+            s[x + "b"] = 0.2 * torch.randn(d, device=DEV, generator=g) if c["kind"] == "layer" else None
+        if c["op"] == "norm":
+            s.update(qo=torch.zeros(B, H, L, d, device=DEV, dtype=torch.bfloat16),
+                     ko=torch.zeros(B, Hkv, L, d, device=DEV, dtype=torch.bfloat16))
+        else:
+            s["gq"], s["gk"] = (0.1 * torch.randn(B, n, L, d, device=DEV, generator=g) for n in (H, Hkv))
+            s["gq"], s["gk"] = s["gq"].to(torch.bfloat16), s["gk"].to(torch.bfloat16)
+            s.update(dq=_like(q), dk=_like(k))
+            s["sums"] = {x: torch.zeros(d, device=DEV) for x in (("qw", "kw") if c["kind"] == "rms" else ("qw", "kw", "qb", "kb"))}
+        return s
+    Hkv, block = c["Hkv"], c["block"]
+    gain = torch.exp(0.5 * torch.randn(2 * Hkv, 1, device=DEV, generator=g))
+    if c["op"] == "cache":
+        held = c["held"]
+        s["start"] = torch.full((B,), held, device=DEV, dtype=torch.int32)
+        if B > 1:
+            s["start"] = torch.randint(0, held + 1, (B,), device=DEV, generator=g, dtype=torch.int32)
+        old = torch.randn(2, B, Hkv, max(held, 1), d, device=DEV, generator=g)
+        s.update(_new_cache(old[0], old[1], block, c["blocks"]))
+        s["k"], s["v"] = _heads(c["packed"], g, B, [Hkv, Hkv], L, d, gain)
+        s["first"] = torch.div(s["start"], block, rounding_mode="floor").to(torch.int32) * block      # where the reading begins
+        s["count"] = s["start"] - s["first"] + L
+        rows = _touched(c) * block
+        s["ko"], s["vo"] = (torch.zeros(B, Hkv, rows, d, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+        return s
+    H, held = c["H"], c["held"]
+    blocks = -(-held // block)
+    kv = torch.randn(2, B, Hkv, held, d, device=DEV, generator=g)
+    kv[0] *= gain[:Hkv].reshape(Hkv, 1, 1).clamp(0.5, 1.5)
+    s.update(_new_cache(kv[0], kv[1], block, blocks))
+    del kv
+    s["length"] = torch.full((B,), held, device=DEV, dtype=torch.int32)
+    if c["ragged"]:
+        s["length"] = torch.randint(1, held + 1, (B,), device=DEV, generator=g, dtype=torch.int32)
+        s["length"][0] = held
+    s["q"], = _heads(c["packed"], g, B, [H], L, d, 1.5)
+    s["row_ptr"] = s["col_idx"] = None
+    if c["kept"] < 1.0:
+        rows = -(-L // block)
+        mask = torch.rand(B, Hkv, rows, blocks, device=DEV, generator=g) < c["kept"]
+        mask[..., 0] = True                                          # every row keeps a block that every sequence has
+        counts = mask.sum(-1).cumsum(-1).to(torch.int32).reshape(B * Hkv, rows)
+        s["row_ptr"] = torch.cat([torch.zeros_like(counts[:, :1]), counts], dim=1).contiguous()
+        s["col_idx"] = torch.full((B * Hkv, rows * blocks), -1, device=DEV, dtype=torch.int32)
+        slab, row, col = mask.reshape(B * Hkv, rows, blocks).nonzero(as_tuple=True)
+        inside = (mask.reshape(B * Hkv, rows * blocks).cumsum(-1) - 1)[slab, row * blocks + col]
+        s["col_idx"][slab, inside] = col.to(torch.int32)
+    s["o"] = _like(s["q"])
+    s["lse"] = torch.zeros(B * H, L, device=DEV)
+    return s
+
+
+def _touched(c):
+    """The blocks that L tokens behind a sequence of any length reach into, at most."""
+    return (c["L"] + c["block"] - 2) // c["block"] + 1
+
+
+# ------------------------------------------------------------------------------------------ one pass
+
+def _angles(s):
+    """cos and sin [B or 1, 1, L, rot / 2] of the call's tokens; a row that the tables do not have turns nothing."""
+    c = s["c"]
+    row = c["first"] + torch.arange(c["L"], device=DEV)[None]
+    if s["start"] is not None:
+        row = row + s["start"][:, None]
+    n = s["cos"].shape[0]
+    there = ((row >= 0) & (row < n))[..., None]
+    at = row.clamp(0, n - 1)
+    cos = torch.where(there, s["cos"][at], torch.ones((), device=DEV))
+    sin = torch.where(there, s["sin"][at], torch.zeros((), device=DEV))
+    return cos[:, None], sin[:, None]
+
+
+def _turn(x, cos, sin, c):
+    """Rotates the first rot channels of x [B, n, L, d] fp32."""
+    r = c["rot"]
+    if c["pairing"] == "adjacent":
+        a, b = x[..., 0:r:2], x[..., 1:r:2]
+        y = torch.stack([a * cos - b * sin, a * sin + b * cos], dim=-1).flatten(-2)
+    else:
+        a, b = x[..., : r // 2], x[..., r // 2: r]
+        y = torch.cat([a * cos - b * sin, a * sin + b * cos], dim=-1)
+    return torch.cat([y, x[..., r:]], dim=-1)
+
+
+def _hat(x, c):
+    """The normalised x and 1 / its deviation."""
+    x = x.float()
+    if c["kind"] == "layer":
+        x = x - x.mean(-1, keepdim=True)
+    r = 1.0 / torch.sqrt((x * x).mean(-1, keepdim=True) + EPS)
+    return x * r, r
+
+
+def _forward(x, w, b, cos, sin, c):
+    z = _hat(x, c)[0] * w
+    if b is not None:
+        z = z + b
+    return _turn(z, cos, sin, c).to(torch.bfloat16)
+
+
+def _backward(x, dy, w, cos, sin, c):
+    dz = _turn(dy.float(), cos, -sin, c)
+    hat, r = _hat(x, c)
+    gw = dz * w
+    dx = gw - hat * (gw * hat).mean(-1, keepdim=True)
+    if c["kind"] == "layer":
+        dx = dx - gw.mean(-1, keepdim=True)
+    return (dx * r).to(torch.bfloat16), (dz * hat).sum((0, 1, 2)), dz.sum((0, 1, 2))
+
+
+def _append(s, x, codes, scales, lay, tokens, out):
+    """One of K, V: the blocks that the new tokens go to are decoded, joined with them, coded again and stored;
+    returns those blocks' values."""
+    c = s["c"]
+    block, n = c["block"], _touched(c)
+    B, Hkv, L, d = x.shape
+    at = s["first"][:, None].long() // block + torch.arange(n, device=DEV)                 # [B, n]
+    at, batch = at.clamp(max=c["blocks"] - 1), torch.arange(B, device=DEV)[:, None]
+    old = codes[batch, :, at].transpose(1, 2)                                              # [B, Hkv, n, ...]
+    old_scale = scales[batch, :, at].transpose(1, 2)                                       # [B, Hkv, n]
+    old_codes = tokens(old).reshape(B, Hkv, n, block, d)
+    pos = (s["first"][:, None] + torch.arange(n * block, device=DEV)).reshape(B, 1, n, block, 1)
+    start = s["start"].reshape(B, 1, 1, 1, 1)
+    held, new = pos < start, (pos >= start) & (pos < start + L)
+    src = (pos - start).clamp(0, L - 1).reshape(B, 1, n * block, 1).expand(B, Hkv, n * block, d)
+    fresh = torch.gather(x, 2, src).float().reshape(B, Hkv, n, block, d)
+    need = _scale_for(_absmax(fresh, (-2, -1), among=new))
+    scale = torch.where(held.any(3).squeeze(-1), torch.maximum(need, old_scale), need)
+    scale = torch.where(new.any(3).squeeze(-1), scale, old_scale)
+    value = torch.where(new, fresh, _value(old_codes) * old_scale[..., None, None]) / scale[..., None, None]
+    stored = torch.where(held | new, _encode(value), old_codes)
+    codes[batch, :, at] = lay(stored).transpose(1, 2)
+    scales[batch, :, at] = scale.transpose(1, 2)
+    value = (_value(stored) * scale[..., None, None]).to(torch.bfloat16)
+    return torch.where(held | new, value, out.reshape(B, Hkv, n, block, d)).reshape(out.shape)
+
+
+def _attention(s):
+    c = s["c"]
+    B, H, Hkv, L, d, block = c["B"], c["H"], c["Hkv"], c["L"], c["d"], c["block"]
+    k, v = (_value(tokens(s[x + "c"])).reshape(B, Hkv, -1, block, d) * s[x + "s"][..., None, None]
+            for x, tokens in (("k", _k_tokens), ("v", _v_tokens)))
+    blocks = k.shape[2]
+    k, v = k.reshape(B, Hkv, -1, d), v.reshape(B, Hkv, -1, d)
+    seen = (torch.arange(blocks * block, device=DEV) < s["length"][:, None])[:, None, None, None]   # [B, 1, 1, 1, keys]
+    if s["row_ptr"] is not None:
+        rows = s["row_ptr"].shape[1] - 1
+        i = torch.arange(rows * blocks, device=DEV)[None]
+        row = torch.searchsorted(s["row_ptr"][:, 1:].contiguous(), i.expand(B * Hkv, -1).to(torch.int32).contiguous(), right=True)
+        kept = torch.zeros(B * Hkv, rows * blocks + 1, device=DEV, dtype=torch.bool)
+        at = torch.where(i < s["row_ptr"][:, -1:], row * blocks + s["col_idx"], rows * blocks)
+        kept.scatter_(1, at.long(), True)
+        kept = kept[:, :-1].reshape(B, Hkv, 1, rows, blocks)
+        kept = kept.repeat_interleave(block, dim=3)[:, :, :, :L].repeat_interleave(block, dim=4)
+        seen = seen & kept
+    q = s["q"].float().reshape(B, Hkv, H // Hkv * L, d)
+    x = torch.matmul(q, k.transpose(-1, -2).contiguous()).mul_(d ** -0.5).reshape(B, Hkv, H // Hkv, L, blocks * block)
+    x = x.masked_fill_(~seen, float("-inf"))
+    m = x.amax(-1, keepdim=True)
+    x = x.sub_(m).exp_()
+    total = x.sum(-1, keepdim=True)
+    o = torch.matmul(x.reshape(B, Hkv, H // Hkv * L, -1), v).reshape(B, H, L, d) / total.reshape(B, H, L, 1)
+    return o.to(torch.bfloat16), (m + torch.log(total)).reshape(B * H, L)
+
+
+def run(state):
+    s = state
+    if own:
+        return _own(s)
+    c = s["c"]
+    if c["op"] == "norm":
+        cos, sin = _angles(s)
+        return {"q": _forward(s["q"], s["qw"], s["qb"], cos, sin, c), "k": _forward(s["k"], s["kw"], s["kb"], cos, sin, c)}
+    if c["op"] == "norm_bwd":
+        cos, sin = _angles(s)
+        dq, qw, qb = _backward(s["q"], s["gq"], s["qw"], cos, sin, c)
+        dk, kw, kb = _backward(s["k"], s["gk"], s["kw"], cos, sin, c)
+        sums = {"qw": qw, "kw": kw} if c["kind"] == "rms" else {"qw": qw, "kw": kw, "qb": qb, "kb": kb}
+        return {"dq": dq, "dk": dk, **sums}
+    if c["op"] == "cache":
+        k = _append(s, s["k"], s["kc"], s["ks"], _k_codes, _k_tokens, s["ko"])
+        v = _append(s, s["v"], s["vc"], s["vs"], _v_codes, _v_tokens, s["vo"])
+        return {"k": k, "v": v, "ks": s["ks"], "vs": s["vs"]}
+    o, lse = _attention(s)
+    return {"o": o, "lse": lse}
+
+
+def _handle(s):
+    """What a program sets up once for its layers and keeps: sizes, strides, parameters, workspace."""
+    from paper_2508_10774_amd import binding as asa
+    c = s["c"]
+    shape = {"B": c["B"], "L": c["L"], "d": c["d"]}
+    if c["op"] in ("norm", "norm_bwd"):
+        p = asa.Params(H=c["H"], block=128, q_stride=s["q"].stride()[:3], k_stride=s["k"].stride()[:3], **shape)
+        n = asa.QkNorm(H_kv=c["Hkv"], kind=c["kind"], eps=EPS, q_weight=s["qw"], k_weight=s["kw"], q_bias=s["qb"], k_bias=s["kb"],
+                       rot_dim=c["rot"], pairing=c["pairing"], cos=s["cos"], sin=s["sin"], first_row=c["first"], start=s["start"])
+        ws = asa.alloc_workspace(asa.asa_qk_norm_rope_bwd_workspace_bytes(p, n)) if c["op"] == "norm_bwd" else None
+        return asa, p, n, ws
+    cache = asa.KvCache(k=s["kc"], v=s["vc"], k_scale=s["ks"], v_scale=s["vs"])
+    if c["op"] == "cache":
+        p = asa.Params(H=c["Hkv"], block=c["block"], k_stride=s["k"].stride()[:3], v_stride=s["v"].stride()[:3], **shape)
+        return asa, p, cache, asa.Params(**{**shape, "L": s["ko"].shape[2]}, H=c["Hkv"], block=c["block"])
+    p = asa.Params(H=c["H"], block=c["block"], q_stride=s["q"].stride()[:3], o_stride=s["o"].stride()[:3], **shape)
+    return asa, p, cache, asa.alloc_workspace(asa.asa_attn_cache_workspace_bytes(p, cache))
+
+
+def _own(s):
+    if "handle" not in s:
+        s["handle"] = _handle(s)
+    op = s["c"]["op"]
+    if op == "norm":
+        asa, p, n, _ = s["handle"]
+        asa.asa_qk_norm_rope(p, n, s["q"], s["k"], s["qo"], s["ko"])
+        return {"q": s["qo"], "k": s["ko"]}
+    if op == "norm_bwd":
+        asa, p, n, ws = s["handle"]
+        sums = s["sums"]
+        asa.asa_qk_norm_rope_bwd(p, n, s["q"], s["k"], s["gq"], s["gk"], s["dq"], s["dk"], sums["qw"], sums["kw"],
+                                 sums.get("qb"), sums.get("kb"), ws)
+        return {"dq": s["dq"], "dk": s["dk"], **sums}
+    if op == "cache":
+        asa, p, cache, read = s["handle"]
+        asa.asa_cache_write(p, cache, s["k"], s["v"], start=s["start"])
+        asa.asa_cache_read(read, cache, s["ko"], s["vo"], start=s["first"], count=s["count"])
+        return {"k": s["ko"], "v": s["vo"], "ks": s["ks"], "vs": s["vs"]}
+    asa, p, cache, ws = s["handle"]
+    asa.asa_attn_cache(p, cache, s["length"], s["q"], s["row_ptr"], s["col_idx"], s["o"], s["lse"], ws)
+    return {"o": s["o"], "lse": s["lse"]}
+
+
+# ------------------------------------------------------------------------------------------ the work
+
+def work(case):
+    c = case
+    B, L, d = c["B"], c["L"], c["d"]
+    if c["op"] in ("norm", "norm_bwd"):
+        rows = B * L * (c["H"] + c["Hkv"])
+        table = min(c["T"] * c["Y"] * c["X"], B * L) * c["rot"] * 4
+        if c["op"] == "norm":
+            return {"bytes": rows * d * 4 + table, "flops": rows * d * 8}
+        return {"bytes": rows * d * 6 + table, "flops": rows * d * 16}
+    Hkv = c["Hkv"]
+    if c["op"] == "cache":
+        # two bytes in and one out for each new value, then one in and two out; a part-filled block's codes once more
+        return {"bytes": 2 * B * Hkv * d * (6 * L + (c["block"] // 2 if c["held"] else 0)), "flops": 2 * B * Hkv * L * d * 4}
+    keys = c["held"] * c["kept"] * ((B + 1) / (2 * B) if c["ragged"] else 1.0)       # of a query, at the mean
+    rows = -(-L // c["block"])
+    reached = c["held"] * (1.0 - (1.0 - c["kept"]) ** rows) * ((B + 1) / (2 * B) if c["ragged"] else 1.0)
+    return {"bytes": B * (2 * Hkv * reached * d + 4 * c["H"] * L * d + 4 * c["H"] * L), "flops": 4 * B * c["H"] * L * keys * d}
+
+
+# ------------------------------------------------------------------------------------------ in 64 bits
+
+def _code_values():
+    """The 256 values of the 8-bit type: sign, 4 bits of exponent (bias 7), 3 of fraction; exponent 15 with fraction 7 is NaN."""
+    out = []
+    for code in range(256):
+        e, f = code >> 3 & 15, code & 7
+        x = float("nan") if e == 15 and f == 7 else (f * 2.0 ** -9 if e == 0 else (8 + f) * 2.0 ** (e - 10))
+        out.append(-x if code & 128 else x)
+    return torch.tensor(out, dtype=torch.float64, device=DEV)
+
+
+def _places(block, d):
+    """Where the code of token t, channel x of a block lies: two index tables [block, d], for K and for V."""
+    t = torch.arange(block, device=DEV)[:, None]
+    x = torch.arange(d, device=DEV)[None]
+    r = t % 32
+    k = t // 32 * (32 * d) + x // 16 * 512 + r * 16 + x % 16
+    v = t // 32 * (32 * d) + x // 32 * 1024 + (r // 4 % 2) * 512 + x % 32 * 16 + r // 8 * 4 + r % 4
+    return k, v
+
+
+def _round8(x):
+    """The nearest value of the 8-bit type, |x| <= 448, ties to even: steps of 2^(exponent - 3), of 2^-9 below 2^-6."""
+    _, e = torch.frexp(x)
+    step = _power((e - 4).clamp(min=-9))
+    return torch.round(x / step) * step
+
+
+def exact(case, seed):
+    c = case
+    s = prepare(c, seed)
+    f64 = torch.float64
+    B, L, d = c["B"], c["L"], c["d"]
+    if c["op"] in ("norm", "norm_bwd"):
+        r = c["rot"]
+        row = c["first"] + torch.arange(L, device=DEV).expand(B, L)
+        if s["start"] is not None:
+            row = row + s["start"].long()[:, None]
+        n = s["cos"].shape[0]
+        unit = torch.complex(s["cos"].double(), s["sin"].double())
+        unit = torch.cat([unit, torch.ones_like(unit[:1])])[torch.where((row < 0) | (row >= n), n, row)][:, None]   # [B, 1, L, r / 2]
+        i = torch.arange(r // 2, device=DEV)
+        lo, hi = (2 * i, 2 * i + 1) if c["pairing"] == "adjacent" else (i, i + r // 2)
+
+        def turned(x, u):
+            z = torch.complex(x[..., lo], x[..., hi]) * u
+            y = x.clone()
+            y[..., lo], y[..., hi] = z.real, z.imag
+            return y
+
+        out = {}
+        for name, x, w, b, dy in (("q", s["q"], s["qw"], s["qb"], s.get("gq")), ("k", s["k"], s["kw"], s["kb"], s.get("gk"))):
+            x = x.to(f64)
+            mean = x.mean(-1, keepdim=True) if c["kind"] == "layer" else torch.zeros((), device=DEV, dtype=f64)
+            dev = ((x - mean).pow(2).sum(-1, keepdim=True) / d + EPS).sqrt()
+            hat = (x - mean) / dev
+            if dy is None:
+                out[name] = turned(hat * w.double() + (0.0 if b is None else b.double()), unit)
+                continue
+            dz = turned(dy.to(f64), unit.conj())
+            up = dz * w.double() / dev
+            dx = up - hat * (up * hat).sum(-1, keepdim=True) / d
+            if c["kind"] == "layer":
+                dx = dx - up.sum(-1, keepdim=True) / d
+                out[name + "b"] = dz.sum(dim=(0, 1, 2))
+            out["d" + name], out[name + "w"] = dx, (dz * hat).sum(dim=(0, 1, 2))
+        return out
+    Hkv, block = c["Hkv"], c["block"]
+    values, places = _code_values(), _places(block, d)
+    if c["op"] == "cache":
+        out = {}
+        starts = s["start"].tolist()
+        for name, place in zip("kv", places):
+            x, scales = s[name].to(f64), s[name + "s"].double()
+            codes = s[name + "c"].reshape(B, Hkv, c["blocks"], block * d)
+            back = s[name + "o"].double()
+            for b, start in enumerate(starts):
+                first = start // block
+                last = (start + L - 1) // block
+                old = values[codes[b, :, first].long()[:, place]] * scales[b, :, first, None, None]      # [Hkv, block, d]
+                joined = torch.zeros(Hkv, (last - first + 1) * block, d, device=DEV, dtype=f64)
+                joined[:, start - first * block: start - first * block + L] = x[b]
+                e = torch.frexp(joined.reshape(Hkv, -1, block * d).abs().amax(-1) / LARGEST)
+                need = torch.where(e.mantissa == 0.5, e.exponent - 1, e.exponent)        # the least e with absmax / 448 <= 2^e
+                need = torch.where(e.mantissa == 0, torch.full_like(need, LEAST_EXP), need).clamp(LEAST_EXP, MOST_EXP)
+                scale = _power(need)
+                held = start - first * block
+                if held:
+                    scale[:, 0] = torch.maximum(scale[:, 0], scales[b, :, first])
+                joined[:, :held] = old[:, :held]
+                each = scale.repeat_interleave(block, dim=1)[..., None]
+                back[b, :, :held + L] = (_round8(joined / each) * each)[:, :held + L]
+                scales[b, :, first:last + 1] = scale
+            out[name], out[name + "s"] = back, scales
+        return out
+    H, held = c["H"], c["held"]
+    o = torch.zeros(B, H, L, d, device=DEV, dtype=f64)
+    lse = torch.zeros(B, H, L, device=DEV, dtype=f64)
+    blocks = -(-held // block)
+    lengths = s["length"].tolist()
+    rows = [list(range(0, L, block))] if c["kept"] < 1.0 else [[0]]
+    ptr = s["row_ptr"].reshape(B, Hkv, -1).tolist() if c["kept"] < 1.0 else None
+    for b in range(B):
+        for h in range(Hkv):
+            kv = [values[s[x + "c"][b, h].reshape(blocks, block * d).long()[:, place]] * s[x + "s"][b, h].double()[:, None, None]
+                  for x, place in zip("kv", places)]
+            k, v = (x.reshape(blocks * block, d) for x in kv)
+            q = s["q"][b].reshape(Hkv, H // Hkv, L, d)[h].to(f64)
+            for t in rows[0]:
+                end = t + block if ptr else L
+                at = torch.arange(lengths[b], device=DEV)
+                if ptr:
+                    i = t // block
+                    mine = s["col_idx"][b * Hkv + h, ptr[b][h][i]:ptr[b][h][i + 1]].long()
+                    at = (mine[:, None] * block + torch.arange(block, device=DEV)).reshape(-1)
+                    at = at[at < lengths[b]]
+                x = torch.matmul(q[:, t:end], k[at].T.contiguous()) / math.sqrt(d)
+                z = torch.logsumexp(x, dim=-1, keepdim=True)
+                heads = slice(h * (H // Hkv), (h + 1) * (H // Hkv))
+                o[b, heads, t:end] = torch.matmul(torch.exp(x - z), v[at])
+                lse[b, heads, t:end] = z[..., 0]
+    return {"o": o, "lse": lse.reshape(B * H, L)}
