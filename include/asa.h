@@ -276,6 +276,134 @@ int asa_reorder_tokens(const asa_params *p, int32_t n_tensors, const void *const
                        void *const *dst, const int64_t *src_stride, const int64_t *dst_stride,
                        const int32_t *index, void *hip_stream);
 
+/*
+ * Norm of queries and keys for each head and their rotation by position, in one pass: what stands
+ * between the projections of an attention layer and asa_build_mask / asa_attn_fwd.  For every
+ * row x of d channels (one token of one head):
+ *   ASA_NORM_RMS    y = x r,            r = 1 / sqrt(mean(x^2) + eps)
+ *   ASA_NORM_LAYER  y = (x - mean(x)) r, r = 1 / sqrt(var(x) + eps)
+ *   z = weight * y + bias
+ *   channel pairs t < rot_dim / 2 of z:  (a, b) -> (a c - b s, a s + b c),
+ *     c = cos_table[row][t], s = sin_table[row][t],  row = first_row + start[b] + l
+ *     ASA_ROPE_ADJACENT  a, b = channels 2 t, 2 t + 1
+ *     ASA_ROPE_HALVES    a, b = channels t, t + rot_dim / 2
+ * A row outside [0, table_rows) turns nothing (first_row = -n: n text tokens in front of the video).
+ * Everything is fp32 until the one rounding of the result to bf16.
+ */
+#define ASA_NORM_RMS 0
+#define ASA_NORM_LAYER 1
+#define ASA_ROPE_ADJACENT 0
+#define ASA_ROPE_HALVES 1
+typedef struct asa_qk_norm {
+  int32_t H_kv;              /* heads of K; 0 = as many as Q                                    */
+  int32_t kind;              /* ASA_NORM_RMS, ASA_NORM_LAYER                                     */
+  float eps;                 /* finite, >= 0                                                    */
+  int32_t rot_dim;           /* channels turned: a multiple of 16, 0 .. d (0: norm alone)       */
+  int32_t pairing;           /* ASA_ROPE_ADJACENT, ASA_ROPE_HALVES                               */
+  int32_t table_rows;        /* rows of the tables (>= 1 unless rot_dim is 0)                    */
+  int32_t first_row;         /* table row of token 0                                             */
+  const int32_t *start;      /* DEVICE [B], added to first_row for each sequence; NULL = zeros   */
+  const float *cos_table, *sin_table;   /* DEVICE [table_rows, rot_dim / 2] fp32                 */
+  const float *q_weight, *k_weight;     /* DEVICE [d] fp32; NULL = ones                          */
+  const float *q_bias, *k_bias;         /* DEVICE [d] fp32, ASA_NORM_LAYER only; NULL = zeros    */
+  int64_t q_out_stride[3], k_out_stride[3];  /* of q_out / dq_out and k_out / dk_out, as in
+                                asa_params; all zero = packed [B, H, L, d], [B, H_kv, L, d]      */
+} asa_qk_norm;
+
+/*
+ * q [B, H, L, d], k [B, H_kv, L, d] bf16 with p's q_stride and k_stride (slices of one projection
+ * [B, L, heads * d], say) -> q_out, k_out bf16.  k = k_out = NULL: queries alone.  Of `p` only
+ * B, H, L, d, q_stride and k_stride have a meaning.  L <= 131 072.  A tensor may be its own output
+ * where the strides agree; any other overlap is undefined.
+ */
+int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k,
+                     void *q_out, void *k_out, void *hip_stream);
+
+/*
+ * Its backward: from q, k (the forward's inputs; nothing else is kept) and the gradients dq_out,
+ * dk_out of the outputs (q_out_stride, k_out_stride)
+ *   dq, dk             bf16, q_stride and k_stride
+ *   dq_weight, dk_weight, dq_bias, dk_bias  [d] fp32, sums over batch, heads and tokens; each may be NULL
+ * Sums are formed in a fixed order: runs of a call repeat bit for bit.  dq may take the place of
+ * q or of dq_out (the same strides), dk that of k or dk_out.  k = dk_out = dk = NULL: queries alone.
+ * The biases' gradients belong to ASA_NORM_LAYER.
+ */
+size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n);
+int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k,
+                         const void *dq_out, const void *dk_out, void *dq, void *dk,
+                         float *dq_weight, float *dk_weight, float *dq_bias, float *dk_bias,
+                         void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Keys and values kept in 8 bits: e4m3 (4 significant bits, largest value 448, no infinity) with one fp32
+ * scale for each block of `block` tokens and key head; a code stands for code value * scale.
+ * Generation that goes on from what was generated (chunk after chunk, token after token) writes
+ * each new token once and attends to all that the cache holds.
+ *
+ * Memory.  Blocks of one (sequence, key head) lie one behind the other; a block is block * d bytes, in
+ * groups of 32 tokens, each in the order in which the matrix cores take it:
+ *   k  [B, H_kv, max_blocks, block/32, d/16, 32, 16]     token t of the group, channel 16 c + x at [c][t][x]
+ *   v  [B, H_kv, max_blocks, block/32, d/32, 2, 32, 16]  token 8 m + 4 h + j, channel 32 c + x at
+ *                                                        [c][h][x][4 m + j]  (m, j < 4; h < 2)
+ *   k_scale, v_scale  [B, H_kv, max_blocks] fp32, positive
+ * Token l of a sequence is token l % block of block l / block.
+ */
+typedef struct asa_kv_cache {
+  int32_t H_kv;              /* key heads                                                        */
+  int32_t max_blocks;        /* room of every sequence in blocks, 1 .. 65 536                    */
+  void *k, *v;               /* DEVICE, 16-byte aligned                                          */
+  float *k_scale, *v_scale;  /* DEVICE                                                           */
+} asa_kv_cache;
+
+/*
+ * Writes p->L new tokens of each sequence, k and v [B, H_kv, L, d] bf16 (k_stride, v_stride; one of
+ * them may be NULL: the other tensor alone), to positions start[b] .. start[b] + count[b] - 1.
+ * start, count: DEVICE [B] int32; NULL = 0, p->L.  Of `p`: B, L, d, block, k_stride, v_stride.
+ * A sequence then ends there: tokens before start[b] are kept, and what lay behind is no longer
+ * part of it (its bytes are left as they were).
+ *   - A block's scale is the least power of two 2^e, -100 <= e <= 120, with |x| <= 448 * 2^e for
+ *     its finite values, and a code is x / scale rounded to nearest, ties to even: the powers of two
+ *     cost e4m3 no precision and make scaling exact.
+ *   - A block that holds tokens before start[b] keeps its scale if that is enough for the new ones;
+ *     otherwise it gets the larger one and the codes held are rounded again to it.
+ *   - NaN and infinities are stored as NaN, and have no part in the scale.
+ *   - Tokens past max_blocks * block are not written; start[b] < 0 writes nothing of that sequence;
+ *     count[b] counts as clamped to [0, L].
+ *   - Blocks that no new token goes to are not touched.
+ */
+int asa_cache_write(const asa_params *p, const asa_kv_cache *c, const void *k, const void *v,
+                    const int32_t *start, const int32_t *count, void *hip_stream);
+
+/*
+ * Reads tokens start[b] .. start[b] + count[b] - 1 of each sequence back into rows 0 .. count[b] - 1 of
+ * k and v [B, H_kv, L, d] bf16 (k_stride, v_stride; one may be NULL): code value * scale, exact up to
+ * bf16's range for the scales that asa_cache_write makes.  Rows from count[b] on, and rows of positions
+ * outside [0, max_blocks * block), are left as they were.  start, count as above.
+ */
+int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v,
+                   const int32_t *start, const int32_t *count, void *hip_stream);
+
+/*
+ * Attention over the cache: q [B, H, L, d] bf16 (q_stride), H a multiple of H_kv; query head h reads
+ * key head h / (H / H_kv).  A query sees the tokens [0, length[b]) of its sequence that lie in the
+ * blocks its list keeps:
+ *   S = scale * q K^T,  LSE = log sum exp S,  O = exp(S - LSE) V,   K, V = code value * scale.
+ * length   DEVICE [B] int32, counts as clamped to [0, max_blocks * block]
+ * row_ptr  [B*H_kv, ceil(L/block) + 1] int32, col_idx [B*H_kv, ceil(L/block) * max_blocks] int32: the
+ *          lists of asa_build_mask, one for each block of queries and KEY head, of distinct blocks in any
+ *          order; entries that are negative or at or past the sequence's last block are skipped.  Both
+ *          NULL: every block.
+ * o        [B, H, L, d] bf16 (o_stride); lse [B*H, L] fp32.  A row that sees nothing gets O = 0, LSE = -inf.
+ * Codes are widened to bf16 (exact), products accumulate in fp32; probabilities, times the block's
+ * scale of V, are rounded to bf16 before the second product.  What the cache holds at and past length[b]
+ * has no influence, whatever the bytes are.  Runs of a call repeat bit for bit.
+ * L = 1 is a token-by-token step.  ceil(L/block) * max_blocks < 2^31.
+ */
+size_t asa_attn_cache_workspace_bytes(const asa_params *p, const asa_kv_cache *c);
+int asa_attn_cache(const asa_params *p, const asa_kv_cache *c, const int32_t *length, const void *q,
+                   const int32_t *row_ptr, const int32_t *col_idx, void *o, float *lse,
+                   void *workspace, size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,9 +36,29 @@ class asa_params(ctypes.Structure):
     ]
 
 
+class asa_qk_norm(ctypes.Structure):
+    _fields_ = [
+        ("H_kv", ctypes.c_int32), ("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("rot_dim", ctypes.c_int32),
+        ("pairing", ctypes.c_int32), ("table_rows", ctypes.c_int32), ("first_row", ctypes.c_int32),
+        ("start", ctypes.c_void_p), ("cos_table", ctypes.c_void_p), ("sin_table", ctypes.c_void_p),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+        ("q_bias", ctypes.c_void_p), ("k_bias", ctypes.c_void_p),
+        ("q_out_stride", ctypes.c_int64 * 3), ("k_out_stride", ctypes.c_int64 * 3),
+    ]
+
+
+class asa_kv_cache(ctypes.Structure):
+    _fields_ = [
+        ("H_kv", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+    ]
+
+
 # The same fields in one call (native sizes and alignment): setting them one by one takes 4 us, as long as a launch.
 _PACKED = struct.Struct("@6iP3fif12q")
 assert _PACKED.size == ctypes.sizeof(asa_params)
+_PACKED_NORM, _PACKED_CACHE = struct.Struct("@2if4i7P6q"), struct.Struct("@2i4P")
+assert _PACKED_NORM.size == ctypes.sizeof(asa_qk_norm) and _PACKED_CACHE.size == ctypes.sizeof(asa_kv_cache)
 
 EXPORTS = ["asa_version", "asa_error_string", "asa_last_hip_error", "asa_mask_workspace_bytes",
            "asa_fwd_workspace_bytes", "asa_bwd_workspace_bytes", "asa_build_mask",
@@ -47,6 +67,8 @@ EXPORTS = ["asa_version", "asa_error_string", "asa_last_hip_error", "asa_mask_wo
            "asa_fwd_g_workspace_bytes", "asa_attn_fwd_g", "asa_bwd_g_workspace_bytes",
            "asa_attn_bwd_g", "asa_mask_seeded_workspace_bytes", "asa_build_mask_seeded",
            "asa_sample_offsets", "asa_gilbert_order", "asa_reorder_tokens",
+           "asa_qk_norm_rope", "asa_qk_norm_rope_bwd_workspace_bytes", "asa_qk_norm_rope_bwd",
+           "asa_cache_write", "asa_cache_read", "asa_attn_cache_workspace_bytes", "asa_attn_cache",
            "asa_mfma_rate_probe", "asa_test_force_fwd_kernel", "asa_add_rate_probe"]
 
 
@@ -92,6 +114,17 @@ def load():
     L.asa_mfma_rate_probe.restype = ctypes.c_int
     L.asa_gilbert_order.argtypes = [ctypes.c_int32] * 4 + [vp, vp]
     L.asa_reorder_tokens.argtypes = [pp, ctypes.c_int32, vp, vp, vp, vp, vp, vp]
+    pn, pc = ctypes.POINTER(asa_qk_norm), ctypes.POINTER(asa_kv_cache)
+    L.asa_qk_norm_rope.argtypes = [pp, pn] + [vp] * 5
+    L.asa_qk_norm_rope_bwd.argtypes = [pp, pn] + [vp] * 11 + [ctypes.c_size_t, vp]
+    L.asa_qk_norm_rope_bwd_workspace_bytes.argtypes = [pp, pn]
+    L.asa_cache_write.argtypes = L.asa_cache_read.argtypes = [pp, pc] + [vp] * 5
+    L.asa_attn_cache.argtypes = [pp, pc] + [vp] * 7 + [ctypes.c_size_t, vp]
+    L.asa_attn_cache_workspace_bytes.argtypes = [pp, pc]
+    for n in ("asa_qk_norm_rope_bwd_workspace_bytes", "asa_attn_cache_workspace_bytes"):
+        getattr(L, n).restype = ctypes.c_size_t
+    for n in ("asa_qk_norm_rope", "asa_qk_norm_rope_bwd", "asa_cache_write", "asa_cache_read", "asa_attn_cache"):
+        getattr(L, n).restype = ctypes.c_int
     for n in ("asa_gilbert_order", "asa_reorder_tokens", "asa_build_mask", "asa_mask_from_scores", "asa_csr_from_mask", "asa_attn_fwd",
               "asa_attn_bwd", "asa_set_kernel_timing", "asa_global_tokens", "asa_attn_fwd_g",
               "asa_attn_bwd_g", "asa_build_mask_seeded", "asa_sample_offsets"):
@@ -329,6 +362,188 @@ def asa_reorder_tokens(p: Params, src, dst, index, src_stride=None, dst_stride=N
                                      _stream(stream)), "asa_reorder_tokens")
 
 
+# ---------------------------------------------------------------------------
+# norm and rotation of queries and keys; keys and values in 8 bits
+# ---------------------------------------------------------------------------
+
+def _device(stream, first: torch.Tensor) -> int:
+    """The device that the call's tensors have to be on: the current one, also for a stream of the caller's."""
+    if not first.is_cuda:
+        raise AsaError("libasa takes device tensors")
+    dev = torch.cuda.current_device()
+    if stream is not None and stream.device_index != dev:
+        raise AsaError("the stream is not one of the current device")
+    return dev
+
+
+def _flat(t: Optional[torch.Tensor], what: str, dtype, n: int, dev: int) -> int:
+    """Pointer of a contiguous tensor of (at least) n elements; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+        raise AsaError(f"{what}: {n} contiguous elements of {dtype} on device {dev} expected, got {tuple(t.shape)} of "
+                       f"{t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(t: Optional[torch.Tensor], what: str, shape, stride, dev: int) -> int:
+    """Pointer of a bf16 tensor [B, heads, L, d] that has the strides that the call gives for it; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not torch.bfloat16 or t.get_device() != dev or tuple(t.shape) != shape:
+        raise AsaError(f"{what}: bf16 {shape} on device {dev} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    B, H, L, d = shape
+    s0, s1, s2 = stride
+    if not (s0 or s1 or s2):
+        s0, s1, s2 = H * L * d, L * d, d
+    got = t.stride()
+    if got != (s0, s1, s2, 1) and any(n > 1 and a != b for n, a, b in zip(shape, got, (s0, s1, s2, 1))):
+        raise AsaError(f"{what}: strides {(s0, s1, s2, 1)} expected, got {got}")
+    return t.data_ptr()
+
+
+_KINDS = {"rms": 0, "layer": 1}
+_PAIRINGS = {"adjacent": 0, "halves": 1}
+
+
+@dataclass
+class QkNorm:
+    """``asa_qk_norm``: the norm of each head's rows, its parameters, the angles of the positions.
+
+    kind "rms" | "layer"; weights and biases [d] fp32 (None: ones, zeros); cos, sin [table_rows, rot_dim / 2] fp32;
+    pairing "adjacent" | "halves"; start [B] int32, added to first_row for each sequence."""
+    H_kv: int = 0
+    kind: str = "rms"
+    eps: float = 1e-6
+    q_weight: Optional[torch.Tensor] = None
+    k_weight: Optional[torch.Tensor] = None
+    q_bias: Optional[torch.Tensor] = None
+    k_bias: Optional[torch.Tensor] = None
+    rot_dim: int = 0
+    pairing: str = "adjacent"
+    cos: Optional[torch.Tensor] = None
+    sin: Optional[torch.Tensor] = None
+    first_row: int = 0
+    start: Optional[torch.Tensor] = None
+    q_out_stride: Sequence[int] = (0, 0, 0)
+    k_out_stride: Sequence[int] = (0, 0, 0)
+
+    def c(self, p: Params, dev: int) -> asa_qk_norm:
+        if self.kind not in _KINDS or self.pairing not in _PAIRINGS:
+            raise AsaError(f"kind {self.kind!r}: one of {list(_KINDS)}; pairing {self.pairing!r}: one of {list(_PAIRINGS)}")
+        f32, d, rows = torch.float32, p.d, 0
+        if self.rot_dim and self.cos is not None and self.sin is not None:
+            rows = min(self.cos.shape[0], self.sin.shape[0])
+            for x in (self.cos, self.sin):
+                if x.dim() != 2 or x.shape[1] * 2 != self.rot_dim:
+                    raise AsaError(f"cos, sin: [rows, {self.rot_dim // 2}] expected, got {tuple(x.shape)}")
+        n = rows * self.rot_dim // 2
+        return asa_qk_norm.from_buffer_copy(_PACKED_NORM.pack(
+            self.H_kv, _KINDS[self.kind], self.eps, self.rot_dim, _PAIRINGS[self.pairing], rows, self.first_row,
+            _flat(self.start, "start", torch.int32, p.B, dev),
+            _flat(self.cos, "cos", f32, n, dev), _flat(self.sin, "sin", f32, n, dev),
+            _flat(self.q_weight, "q_weight", f32, d, dev), _flat(self.k_weight, "k_weight", f32, d, dev),
+            _flat(self.q_bias, "q_bias", f32, d, dev), _flat(self.k_bias, "k_bias", f32, d, dev),
+            *self.q_out_stride, *self.k_out_stride))
+
+
+def asa_qk_norm_rope(p: Params, n: QkNorm, q, k, q_out, k_out, stream=None):
+    """q [B, H, L, d], k [B, H_kv, L, d] -> q_out, k_out: norm for each head, then rotation (k = k_out = None: q alone)."""
+    dev = _device(stream, q)
+    qs, ks = (p.B, p.H, p.L, p.d), (p.B, n.H_kv or p.H, p.L, p.d)
+    _check(load().asa_qk_norm_rope(ctypes.byref(p.c()), ctypes.byref(n.c(p, dev)), _rows(q, "q", qs, p.q_stride, dev),
+                                   _rows(k, "k", ks, p.k_stride, dev), _rows(q_out, "q_out", qs, n.q_out_stride, dev),
+                                   _rows(k_out, "k_out", ks, n.k_out_stride, dev), _stream(stream)), "asa_qk_norm_rope")
+
+
+def asa_qk_norm_rope_bwd_workspace_bytes(p: Params, n: QkNorm) -> int:
+    """Depends on p's sizes and strides and on n.H_kv."""
+    c = asa_qk_norm(H_kv=n.H_kv)
+    return int(load().asa_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(p.c()), ctypes.byref(c)))
+
+
+def asa_qk_norm_rope_bwd(p: Params, n: QkNorm, q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, dq_bias, dk_bias,
+                         workspace, stream=None):
+    dev = _device(stream, q)
+    qs, ks = (p.B, p.H, p.L, p.d), (p.B, n.H_kv or p.H, p.L, p.d)
+    f32, d = torch.float32, p.d
+    _check(load().asa_qk_norm_rope_bwd(
+        ctypes.byref(p.c()), ctypes.byref(n.c(p, dev)), _rows(q, "q", qs, p.q_stride, dev), _rows(k, "k", ks, p.k_stride, dev),
+        _rows(dq_out, "dq_out", qs, n.q_out_stride, dev), _rows(dk_out, "dk_out", ks, n.k_out_stride, dev),
+        _rows(dq, "dq", qs, p.q_stride, dev), _rows(dk, "dk", ks, p.k_stride, dev),
+        _flat(dq_weight, "dq_weight", f32, d, dev), _flat(dk_weight, "dk_weight", f32, d, dev),
+        _flat(dq_bias, "dq_bias", f32, d, dev), _flat(dk_bias, "dk_bias", f32, d, dev),
+        _flat(workspace, "workspace", torch.uint8, 0, dev), workspace.nbytes if workspace is not None else 0,
+        _stream(stream)), "asa_qk_norm_rope_bwd")
+
+
+@dataclass
+class KvCache:
+    """``asa_kv_cache``: the tensors of ``alloc_kv_cache`` (k [B, H_kv, max_blocks, block/32, d/16, 32, 16] and
+    v [B, H_kv, max_blocks, block/32, d/32, 2, 32, 16] uint8, the scales [B, H_kv, max_blocks] fp32)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    @property
+    def H_kv(self) -> int:
+        return self.k_scale.shape[1]
+
+    @property
+    def max_blocks(self) -> int:
+        return self.k_scale.shape[2]
+
+    def c(self, p: Params, dev: int) -> asa_kv_cache:
+        B, H, blocks = self.k_scale.shape
+        if B != p.B or self.v_scale.shape != self.k_scale.shape:
+            raise AsaError(f"cache of {tuple(self.k_scale.shape)} and {tuple(self.v_scale.shape)} blocks for {p.B} sequences")
+        n = B * H * blocks
+        codes = n * p.block * p.d
+        if self.k.numel() != codes or self.v.numel() != codes:
+            raise AsaError(f"cache: {codes} codes expected, got {self.k.numel()} and {self.v.numel()}")
+        return asa_kv_cache.from_buffer_copy(_PACKED_CACHE.pack(
+            H, blocks, _flat(self.k, "cache.k", torch.uint8, codes, dev), _flat(self.v, "cache.v", torch.uint8, codes, dev),
+            _flat(self.k_scale, "cache.k_scale", torch.float32, n, dev),
+            _flat(self.v_scale, "cache.v_scale", torch.float32, n, dev)))
+
+
+def _cache_call(fn, p: Params, c: KvCache, k, v, start, count, stream):
+    dev = _device(stream, c.k)
+    shape = (p.B, c.H_kv, p.L, p.d)
+    _check(getattr(load(), fn)(ctypes.byref(p.c()), ctypes.byref(c.c(p, dev)), _rows(k, "k", shape, p.k_stride, dev),
+                               _rows(v, "v", shape, p.v_stride, dev), _flat(start, "start", torch.int32, p.B, dev),
+                               _flat(count, "count", torch.int32, p.B, dev), _stream(stream)), fn)
+
+
+def asa_cache_write(p: Params, c: KvCache, k, v, start=None, count=None, stream=None):
+    """New tokens k, v [B, H_kv, L, d] to positions start[b] .. start[b] + count[b] - 1 (None: 0, L) of each sequence."""
+    _cache_call("asa_cache_write", p, c, k, v, start, count, stream)
+
+
+def asa_cache_read(p: Params, c: KvCache, k, v, start=None, count=None, stream=None):
+    """Those positions back into rows 0 .. count[b] - 1 of k, v [B, H_kv, L, d] bf16."""
+    _cache_call("asa_cache_read", p, c, k, v, start, count, stream)
+
+
+def asa_attn_cache_workspace_bytes(p: Params, c: KvCache) -> int:
+    """Depends on p's sizes and strides and on the cache's heads and blocks (0: no workspace needed)."""
+    s = asa_kv_cache(H_kv=c.H_kv, max_blocks=c.max_blocks)
+    return int(load().asa_attn_cache_workspace_bytes(ctypes.byref(p.c()), ctypes.byref(s)))
+
+
+def asa_attn_cache(p: Params, c: KvCache, length, q, row_ptr, col_idx, o, lse, workspace, stream=None):
+    """q [B, H, L, d] attends to tokens [0, length[b]) of the cache, in the blocks of the lists if there are any."""
+    dev = _device(stream, q)
+    shape, lists = (p.B, p.H, p.L, p.d), p.B * c.H_kv
+    _check(load().asa_attn_cache(
+        ctypes.byref(p.c()), ctypes.byref(c.c(p, dev)), _flat(length, "length", torch.int32, p.B, dev),
+        _rows(q, "q", shape, p.q_stride, dev), _flat(row_ptr, "row_ptr", torch.int32, lists * (p.Nb + 1), dev),
+        _flat(col_idx, "col_idx", torch.int32, lists * p.Nb * c.max_blocks, dev), _rows(o, "o", shape, p.o_stride, dev),
+        _flat(lse, "lse", torch.float32, p.B * p.H * p.L, dev), _flat(workspace, "workspace", torch.uint8, 0, dev),
+        workspace.nbytes if workspace is not None else 0, _stream(stream)), "asa_attn_cache")
+
+
 def asa_mfma_rate_probe(workgroups: int, iters: int, sink, idle_sleep: int = 0, vector_stream: bool = False,
                         stream=None) -> float:
     """Launch the MFMA-only calibration kernel; returns the FLOP of the launch."""
@@ -366,3 +581,12 @@ def alloc_index_lists(p: Params, device="cuda", with_csc: bool = True):
 
 def alloc_workspace(nbytes: int, device="cuda") -> torch.Tensor:
     return torch.empty((max(int(nbytes), 256),), dtype=torch.uint8, device=device)
+
+
+def alloc_kv_cache(B: int, H_kv: int, max_blocks: int, d: int, block: int, device="cuda") -> KvCache:
+    """An empty cache: room for max_blocks * block tokens of each sequence."""
+    lead = (B, H_kv, max_blocks)
+    return KvCache(k=torch.zeros(*lead, block // 32, d // 16, 32, 16, dtype=torch.uint8, device=device),
+                   v=torch.zeros(*lead, block // 32, d // 32, 2, 32, 16, dtype=torch.uint8, device=device),
+                   k_scale=torch.ones(lead, dtype=torch.float32, device=device),
+                   v_scale=torch.ones(lead, dtype=torch.float32, device=device))

@@ -10,6 +10,7 @@
 #include "asa_bench.h"
 
 #include "asa_common.hpp"
+#include "asa_extra.hpp"
 
 namespace asa {
 
@@ -564,6 +565,188 @@ int asa_reorder_tokens(const asa_params *p, int32_t n_tensors, const void *const
     return ASA_ERR_INVALID_ARG;
   return finish(launch_reorder(pb, n_tensors, src, dst, ts, td, index,
                                reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+// ------------------------------------------------------------------ norm and rotation of queries and keys
+// The shape of a call that has only B, H, L, d (and block) of asa_params; strides are looked at apart.
+static int resolve_shape(const asa_params *p, int H, int block, Problem *pb) {
+  if (!p) return ASA_ERR_INVALID_ARG;
+  asa_params shape;
+  memset(&shape, 0, sizeof(shape));
+  shape.B = p->B; shape.H = H; shape.L = p->L; shape.d = p->d;
+  shape.block = block; shape.k_samples = 1; shape.tau = 0.5f; shape.r_max = 1.f;
+  return resolve(&shape, pb);
+}
+
+static int check_norm(const asa_params *p, const asa_qk_norm *n, NormArgs *a) {
+  if (!p || !n) return ASA_ERR_INVALID_ARG;
+  Problem q, k;
+  int rc = resolve_shape(p, p->H, 128, &q);
+  if (rc != ASA_OK) return rc;
+  if (n->H_kv < 0) return ASA_ERR_INVALID_ARG;
+  rc = resolve_shape(p, n->H_kv ? n->H_kv : p->H, 128, &k);
+  if (rc != ASA_OK) return rc;
+  if (n->kind != ASA_NORM_RMS && n->kind != ASA_NORM_LAYER) return ASA_ERR_INVALID_ARG;
+  if (!(n->eps >= 0.f) || isinf(n->eps)) return ASA_ERR_INVALID_ARG;
+  if (n->rot_dim < 0 || n->rot_dim > p->d || n->rot_dim % 16) return ASA_ERR_INVALID_ARG;
+  if (n->rot_dim) {
+    if (n->pairing != ASA_ROPE_ADJACENT && n->pairing != ASA_ROPE_HALVES) return ASA_ERR_INVALID_ARG;
+    if (n->table_rows < 1 || !n->cos_table || !n->sin_table || !aligned16(n->cos_table) || !aligned16(n->sin_table))
+      return ASA_ERR_INVALID_ARG;
+  }
+  if (!aligned4(n->start) || !aligned4(n->q_weight) || !aligned4(n->k_weight) || !aligned4(n->q_bias) || !aligned4(n->k_bias))
+    return ASA_ERR_INVALID_ARG;
+  if (n->kind == ASA_NORM_RMS && (n->q_bias || n->k_bias)) return ASA_ERR_INVALID_ARG;
+  memset(a, 0, sizeof(*a));
+  if (!view_from(p->q_stride, q, &a->side[0].in) || !view_from(n->q_out_stride, q, &a->side[0].out) ||
+      !view_from(p->k_stride, k, &a->side[1].in) || !view_from(n->k_out_stride, k, &a->side[1].out))
+    return ASA_ERR_INVALID_ARG;
+  a->side[0].heads = q.H; a->side[0].w = n->q_weight; a->side[0].b = n->q_bias;
+  a->side[1].heads = k.H; a->side[1].w = n->k_weight; a->side[1].b = n->k_bias;
+  a->start = n->start; a->cos_table = n->cos_table; a->sin_table = n->sin_table;
+  a->B = p->B; a->L = p->L;
+  a->rot = n->rot_dim; a->table_rows = n->table_rows; a->first_row = n->first_row; a->eps = n->eps;
+  return ASA_OK;
+}
+
+int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k, void *q_out, void *k_out,
+                     void *hip_stream) {
+  NormArgs a;
+  int rc = check_norm(p, n, &a);
+  if (rc != ASA_OK) return rc;
+  if (!q || !q_out || (k == nullptr) != (k_out == nullptr)) return ASA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return ASA_ERR_INVALID_ARG;
+  if (!k) a.side[1].heads = 0;
+  a.side[0].src = q; a.side[0].dst = q_out;
+  a.side[1].src = k; a.side[1].dst = k_out;
+  rc = plan_norm(&a, p->d);
+  if (rc != ASA_OK) return rc;
+  return finish(launch_norm(a, p->d, n->kind == ASA_NORM_LAYER, n->pairing, false, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n) {
+  NormArgs a;
+  if (check_norm(p, n, &a) != ASA_OK || plan_norm(&a, p->d) != ASA_OK) return 0;
+  return round256(norm_partial_bytes(a.side[0], p->d)) + round256(norm_partial_bytes(a.side[1], p->d));
+}
+
+int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k, const void *dq_out,
+                         const void *dk_out, void *dq, void *dk, float *dq_weight, float *dk_weight, float *dq_bias,
+                         float *dk_bias, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  NormArgs a;
+  int rc = check_norm(p, n, &a);
+  if (rc != ASA_OK) return rc;
+  if (!q || !dq_out || !dq || (k == nullptr) != (dk_out == nullptr) || (k == nullptr) != (dk == nullptr))
+    return ASA_ERR_INVALID_ARG;
+  if (!k && (dk_weight || dk_bias)) return ASA_ERR_INVALID_ARG;
+  if (n->kind == ASA_NORM_RMS && (dq_bias || dk_bias)) return ASA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(dq_out) || !aligned16(dk_out) || !aligned16(dq) || !aligned16(dk) ||
+      !aligned4(dq_weight) || !aligned4(dk_weight) || !aligned4(dq_bias) || !aligned4(dk_bias))
+    return ASA_ERR_INVALID_ARG;
+  if (!k) a.side[1].heads = 0;
+  rc = plan_norm(&a, p->d);
+  if (rc != ASA_OK) return rc;
+  const size_t q_bytes = round256(norm_partial_bytes(a.side[0], p->d)), k_bytes = round256(norm_partial_bytes(a.side[1], p->d));
+  if (!workspace || workspace_bytes < q_bytes + k_bytes || !aligned16(workspace)) return ASA_ERR_WORKSPACE;
+  char *ws = reinterpret_cast<char *>(workspace);
+  a.side[0].src = q; a.side[0].grad = dq_out; a.side[0].dst = dq; a.side[0].dw = dq_weight; a.side[0].db = dq_bias;
+  a.side[1].src = k; a.side[1].grad = dk_out; a.side[1].dst = dk; a.side[1].dw = dk_weight; a.side[1].db = dk_bias;
+  a.side[0].partial = reinterpret_cast<float *>(ws);
+  a.side[1].partial = reinterpret_cast<float *>(ws + q_bytes);
+  return finish(launch_norm(a, p->d, n->kind == ASA_NORM_LAYER, n->pairing, true, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+// ------------------------------------------------------------------ the 8-bit cache
+static int check_cache(const asa_params *p, const asa_kv_cache *c, bool need_k, bool need_v) {
+  if (!p || !c) return ASA_ERR_INVALID_ARG;
+  if (c->H_kv < 1 || c->max_blocks < 1) return ASA_ERR_INVALID_ARG;
+  if (c->max_blocks > 65536) return ASA_ERR_UNSUPPORTED;
+  if ((need_k && (!c->k || !c->k_scale)) || (need_v && (!c->v || !c->v_scale))) return ASA_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned4(c->k_scale) || !aligned4(c->v_scale)) return ASA_ERR_INVALID_ARG;
+  return ASA_OK;
+}
+
+static int cache_args(const asa_params *p, const asa_kv_cache *c, const void *k, const void *v, const int32_t *start,
+                      const int32_t *count, CacheArgs *a) {
+  int rc = check_cache(p, c, k != nullptr, v != nullptr);
+  if (rc != ASA_OK) return rc;
+  Problem pb;
+  rc = resolve_shape(p, c->H_kv, p->block, &pb);
+  if (rc != ASA_OK) return rc;
+  if ((!k && !v) || !aligned16(k) || !aligned16(v) || !aligned4(start) || !aligned4(count)) return ASA_ERR_INVALID_ARG;
+  memset(a, 0, sizeof(*a));
+  TensorView kv, vv;
+  if (!view_from(p->k_stride, pb, &kv) || !view_from(p->v_stride, pb, &vv)) return ASA_ERR_INVALID_ARG;
+  if (k) a->side[a->n_sides++] = CacheSide{c->k, c->k_scale, const_cast<void *>(k), kv, false};
+  if (v) a->side[a->n_sides++] = CacheSide{c->v, c->v_scale, const_cast<void *>(v), vv, true};
+  a->start = start; a->count = count;
+  a->B = pb.B; a->H = pb.H; a->L = pb.L; a->max_blocks = c->max_blocks;
+  // without `start` every sequence begins at a block's first token
+  a->reached = start ? (pb.L + pb.block - 2) / pb.block + 1 : pb.Nb;
+  if (a->reached > c->max_blocks) a->reached = c->max_blocks;
+  if ((int64_t)a->reached * a->H * a->B * a->n_sides >= ((int64_t)1 << 31)) return ASA_ERR_UNSUPPORTED;
+  return ASA_OK;
+}
+
+int asa_cache_write(const asa_params *p, const asa_kv_cache *c, const void *k, const void *v, const int32_t *start,
+                    const int32_t *count, void *hip_stream) {
+  CacheArgs a;
+  int rc = cache_args(p, c, k, v, start, count, &a);
+  if (rc != ASA_OK) return rc;
+  return finish(launch_cache_write(a, p->d, p->block, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v, const int32_t *start, const int32_t *count,
+                   void *hip_stream) {
+  CacheArgs a;
+  int rc = cache_args(p, c, k, v, start, count, &a);
+  if (rc != ASA_OK) return rc;
+  return finish(launch_cache_read(a, p->d, p->block, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+static int check_cache_attn(const asa_params *p, const asa_kv_cache *c, Problem *pb, CacheAttnPlan *plan) {
+  if (!p || !c) return ASA_ERR_INVALID_ARG;
+  int rc = resolve_shape(p, p->H, p->block, pb);
+  if (rc != ASA_OK) return rc;
+  if (p->scale != p->scale || p->scale < 0.f || isinf(p->scale)) return ASA_ERR_INVALID_ARG;
+  pb->scale = p->scale == 0.f ? 1.0f / sqrtf((float)p->d) : p->scale;
+  if (!view_from(p->q_stride, *pb, &pb->q) || !view_from(p->o_stride, *pb, &pb->o)) return ASA_ERR_INVALID_ARG;
+  if (c->H_kv < 1 || c->max_blocks < 1 || pb->H % c->H_kv) return ASA_ERR_INVALID_ARG;
+  if (c->max_blocks > 65536) return ASA_ERR_UNSUPPORTED;
+  return plan_cache_attn(*pb, c->H_kv, c->max_blocks, plan);
+}
+
+size_t asa_attn_cache_workspace_bytes(const asa_params *p, const asa_kv_cache *c) {
+  Problem pb;
+  CacheAttnPlan plan;
+  if (check_cache_attn(p, c, &pb, &plan) != ASA_OK) return 0;
+  return round256(cache_attn_workspace_bytes(pb, plan));
+}
+
+int asa_attn_cache(const asa_params *p, const asa_kv_cache *c, const int32_t *length, const void *q, const int32_t *row_ptr,
+                   const int32_t *col_idx, void *o, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  Problem pb;
+  CacheAttnPlan plan;
+  int rc = check_cache_attn(p, c, &pb, &plan);
+  if (rc != ASA_OK) return rc;
+  rc = check_cache(p, c, true, true);
+  if (rc != ASA_OK) return rc;
+  if (!length || !q || !o || !lse || (row_ptr == nullptr) != (col_idx == nullptr)) return ASA_ERR_INVALID_ARG;
+  if (!aligned4(length) || !aligned16(q) || !aligned16(o) || !aligned4(lse) || !aligned4(row_ptr) || !aligned4(col_idx))
+    return ASA_ERR_INVALID_ARG;
+  const size_t need = round256(cache_attn_workspace_bytes(pb, plan));
+  if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return ASA_ERR_WORKSPACE;
+  CacheAttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = q; a.k = c->k; a.v = c->v; a.k_scale = c->k_scale; a.v_scale = c->v_scale;
+  a.length = length; a.row_ptr = row_ptr; a.col_idx = col_idx; a.o = o; a.lse = lse;
+  a.partial = reinterpret_cast<float *>(workspace);
+  a.qv = pb.q; a.ov = pb.o;
+  a.B = pb.B; a.H = pb.H; a.H_kv = c->H_kv; a.group = pb.H / c->H_kv; a.L = pb.L; a.block = pb.block;
+  a.max_blocks = c->max_blocks; a.n_qblocks = plan.n_qblocks; a.tiles = plan.tiles; a.tile_rows = plan.tile_rows;
+  a.rows_kept = plan.rows_kept; a.splits = plan.splits;
+  a.scale_log2 = pb.scale * 1.4426950408889634f;
+  return finish(launch_cache_attn(a, pb.d, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 int asa_mfma_rate_probe(int32_t workgroups, int32_t iters, int32_t idle_sleep, int32_t vector_stream,

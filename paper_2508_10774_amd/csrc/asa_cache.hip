@@ -1,0 +1,780 @@
+// Keys and values in 8 bits: writing tokens into the cache, reading them back, attention over it
+// (asa_cache_write, asa_cache_read, asa_attn_cache).
+//
+// The cache lies in memory in the order in which the matrix instructions take their operands (asa.h): 32 tokens
+// are D / 32 operand tiles of K and as many of V, 1 KB each, of which a lane takes 16 consecutive bytes.  A
+// wavefront's load is one contiguous KB, from global memory or from LDS, without a swizzle and without a transposition.
+//   K tile t: lane (h, r) holds token r, channels 32 t + 16 h .. + 15: two A operands of S^T = K Q^T, whose result gives
+//             lane (h, query) the tokens 8 m + 4 h + j in register 4 m + j;
+//   V tile t: lane (h, r) holds channel 32 t + r, tokens 8 m + 4 h + j in byte 4 m + j: two A operands of O^T = V^T P^T,
+//             for which the registers of S^T are the B operand as they stand.
+#include "asa_common.hpp"
+#include "asa_extra.hpp"
+#include "asa_tiles.hpp"
+
+namespace asa {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kLeastExp = -100, kMostExp = 120;     // of a block's scale
+
+// A sequence's share [from, to) of the positions of one call, inside the cache.
+struct Span {
+  int64_t from, to;
+};
+__device__ __forceinline__ Span span_of(const CacheArgs &a, int b, int block) {
+  const int64_t start = a.start ? a.start[b] : 0;
+  const int count = a.count ? min(max(a.count[b], 0), a.L) : a.L;
+  const int64_t room = (int64_t)a.max_blocks * block;
+  return Span{start, start + count < room ? start + count : room};
+}
+
+// One (side, sequence, key head, block of the cache) of a call, and the tokens [lo, hi) of it that the call deals with.
+struct BlockItem {
+  int side, b, h, j, lo, hi;
+  int64_t row0;     // row of the call's tensor that token 0 of the block would be
+  bool any;
+};
+__device__ __forceinline__ BlockItem block_item(const CacheArgs &a, int block, bool writing) {
+  BlockItem it;
+  int x = blockIdx.x;
+  const int jb = x % a.reached;
+  x /= a.reached;
+  it.h = x % a.H;
+  x /= a.H;
+  it.b = x % a.B;
+  it.side = x / a.B;
+  const Span s = span_of(a, it.b, block);
+  const int64_t from = s.from < 0 ? 0 : s.from;
+  const int64_t j = from / block + jb, t0 = j * block;
+  it.j = (int)j;
+  it.row0 = t0 - s.from;
+  it.lo = from > t0 ? (int)(from - t0) : 0;
+  it.hi = s.to - t0 < block ? (int)(s.to > t0 ? s.to - t0 : 0) : block;
+  it.any = it.lo < it.hi && !(writing && s.from < 0);
+  return it;
+}
+
+__device__ __forceinline__ uint32_t magnitudes_max(uint32_t a, uint32_t b) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+  const u16x2 x = __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b));
+  return __builtin_bit_cast(uint32_t, x);
+}
+__device__ __forceinline__ bool finite_bits(uint32_t magnitude) { return magnitude < 0x7f80u; }
+
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+#else
+  return 0;
+#endif
+}
+__device__ __forceinline__ f32x4 decode4(uint32_t codes) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+  return f32x4{lo[0], lo[1], hi[0], hi[1]};
+#else
+  return f32x4{};
+#endif
+}
+
+// x / scale: exact by the reciprocal where the scale is a power of two, as those of the writer are
+struct Divider {
+  float scale, reciprocal;
+  bool exact;
+  __device__ __forceinline__ explicit Divider(float s) : scale(s) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, s), e = bits >> 23;
+    exact = (bits & 0x7fffffu) == 0 && e >= 1 && e <= 253;
+    reciprocal = exact ? __builtin_bit_cast(float, (254u - e) << 23) : 0.f;
+  }
+  __device__ __forceinline__ float operator()(float x) const { return exact ? x * reciprocal : x / scale; }
+};
+
+// bytes of a dword whose tokens t0 .. t0 + 3 lie in [lo, hi)
+__device__ __forceinline__ uint32_t bytes_within(int t0, int lo, int hi) {
+  const int a = min(max(lo - t0, 0), 4), b = min(max(hi - t0, 0), 4);
+  return (uint32_t)(((1ull << (8 * b)) - 1) & ~((1ull << (8 * a)) - 1));
+}
+
+// byte address, in a block, of (token, 8 channels from 8 * chunk) in K's order, and of the dword of tokens
+// 4 * quad .. + 3 of one channel in V's
+template <int D>
+__device__ __forceinline__ int k_place(int token, int chunk) {
+  return token / 32 * (32 * D) + chunk / 2 * 512 + token % 32 * 16 + chunk % 2 * 8;
+}
+template <int D>
+__device__ __forceinline__ int v_place(int quad, int channel) {
+  return quad / 8 * (32 * D) + channel / 32 * 1024 + quad % 2 * 512 + channel % 32 * 16 + quad % 8 / 2 * 4;
+}
+
+}  // namespace
+
+// One workgroup for each block that new tokens go to: the rows come in 16 bytes to a lane (four tokens of 8
+// channels in each thread), the block's maximum gives the scale, the codes are put into their order in LDS and leave
+// 16 bytes to a lane.  Bytes of a block that are not new are read only where they share 16 bytes with
+// new ones, or where the scale grew and the tokens held are coded again.
+template <int D, int BLOCK>
+__global__ __launch_bounds__(kThreads) void cache_write_kernel(const CacheArgs a) {
+  constexpr int kChunks = D / 8, kUnits = BLOCK / 4 * kChunks, kPer = (kUnits + kThreads - 1) / kThreads;
+  const BlockItem it = block_item(a, BLOCK, true);
+  if (!it.any) return;
+  const CacheSide &side = a.side[it.side];
+  const int64_t slab = (int64_t)it.b * a.H + it.h;
+  float *scale_at = side.scale + slab * a.max_blocks + it.j;
+  unsigned char *codes = reinterpret_cast<unsigned char *>(side.codes) + (slab * a.max_blocks + it.j) * (BLOCK * D);
+  const bf16 *rows = reinterpret_cast<const bf16 *>(side.rows) + it.b * side.view.sB + it.h * side.view.sH;
+  const bool held = it.lo > 0;
+  const float old_scale = held ? *scale_at : 0.f;
+
+  u32x4 raw[kPer][4];
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int u = threadIdx.x + i * kThreads, quad = u / kChunks, chunk = u % kChunks;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t = quad * 4 + j;
+      raw[i][j] = u32x4{0, 0, 0, 0};
+      if (u < kUnits && t >= it.lo && t < it.hi)
+        raw[i][j] = *reinterpret_cast<const u32x4 *>(rows + (it.row0 + t) * side.view.sL + chunk * 8);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) most = magnitudes_max(most, raw[i][j][w] & 0x7fff7fffu);
+  const bool odd = !finite_bits(most & 0xffffu) || !finite_bits(most >> 16);     // an infinity or a NaN among mine
+  uint32_t top = max(most & 0xffffu, most >> 16);
+  if (odd) {
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t lo = raw[i][j][w] & 0x7fffu, hi = raw[i][j][w] >> 16 & 0x7fffu;
+          if (finite_bits(lo)) top = max(top, lo);
+          if (finite_bits(hi)) top = max(top, hi);
+        }
+  }
+  __shared__ uint32_t wave_top[kThreads / 64];
+  __shared__ __align__(16) unsigned char image[BLOCK * D];
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s, 64));
+  if (threadIdx.x % 64 == 0) wave_top[threadIdx.x / 64] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) top = max(top, wave_top[w]);
+
+  // top = (1 + f) 2^x with f in its low 7 bits; 448 = (1 + 3/4) 2^8
+  int e = (int)(top >> 7) - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
+  e = min(max(e, kLeastExp), kMostExp);
+  const float needed = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
+  const float scale = held && old_scale > needed ? old_scale : needed;
+  const bool recode = held && scale != old_scale;
+  const Divider by(scale);
+
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int u = threadIdx.x + i * kThreads, quad = u / kChunks, chunk = u % kChunks;
+    if (u >= kUnits) break;
+    float x[4][8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        float lo = __builtin_bit_cast(float, raw[i][j][w] << 16), hi = __builtin_bit_cast(float, raw[i][j][w] & 0xffff0000u);
+        if (odd) {
+          if (__builtin_isinf(lo)) lo = __builtin_nanf("");
+          if (__builtin_isinf(hi)) hi = __builtin_nanf("");
+        }
+        x[j][2 * w] = by(lo);
+        x[j][2 * w + 1] = by(hi);
+      }
+    if (side.transposed) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        *reinterpret_cast<uint32_t *>(image + v_place<D>(quad, chunk * 8 + c)) = encode4(x[0][c], x[1][c], x[2][c], x[3][c]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t *to = reinterpret_cast<uint32_t *>(image + k_place<D>(quad * 4 + j, chunk));
+        to[0] = encode4(x[j][0], x[j][1], x[j][2], x[j][3]);
+        to[1] = encode4(x[j][4], x[j][5], x[j][6], x[j][7]);
+      }
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) *scale_at = scale;
+
+  constexpr int kPieces = BLOCK * D / 16;
+#pragma unroll
+  for (int i = 0; i < (kPieces + kThreads - 1) / kThreads; ++i) {
+    const int piece = threadIdx.x + i * kThreads;
+    if (piece >= kPieces) break;
+    const int t_first = piece / (2 * D) * 32 + (side.transposed ? piece / 32 % 2 * 4 : piece % 32);
+    uint32_t fresh[4], again[4], all = ~0u, any = 0;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      // (a piece of K is 16 channels of one token)
+      fresh[m] = side.transposed ? bytes_within(t_first + 8 * m, it.lo, it.hi)
+                                 : (t_first >= it.lo && t_first < it.hi ? ~0u : 0u);
+      again[m] = !recode ? 0u : side.transposed ? bytes_within(t_first + 8 * m, 0, it.lo) : (t_first < it.lo ? ~0u : 0u);
+      all &= fresh[m];
+      any |= fresh[m] | again[m];
+    }
+    if (!any) continue;
+    u32x4 *at = reinterpret_cast<u32x4 *>(codes + piece * 16);
+    u32x4 value = *reinterpret_cast<const u32x4 *>(image + piece * 16);
+    if (all != ~0u) {
+      const u32x4 old = *at;
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        uint32_t kept = old[m];
+        if (again[m]) {
+          const f32x4 was = decode4(old[m]);
+          const uint32_t now = encode4(by(was[0] * old_scale), by(was[1] * old_scale), by(was[2] * old_scale), by(was[3] * old_scale));
+          kept = (now & again[m]) | (kept & ~again[m]);
+        }
+        value[m] = (value[m] & fresh[m]) | (kept & ~fresh[m]);
+      }
+    }
+    *at = value;
+  }
+}
+
+// One workgroup for each block that the call reads from; a thread writes 16 bytes of a row (K) or of four rows (V).
+template <int D, int BLOCK>
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(const CacheArgs a) {
+  constexpr int kChunks = D / 8;
+  const BlockItem it = block_item(a, BLOCK, false);
+  if (!it.any) return;
+  const CacheSide &side = a.side[it.side];
+  const int64_t slab = (int64_t)it.b * a.H + it.h;
+  const float scale = side.scale[slab * a.max_blocks + it.j];
+  const unsigned char *codes = reinterpret_cast<const unsigned char *>(side.codes) + (slab * a.max_blocks + it.j) * (BLOCK * D);
+  bf16 *rows = reinterpret_cast<bf16 *>(side.rows) + it.b * side.view.sB + it.h * side.view.sH;
+  if (side.transposed) {
+    constexpr int kUnits = BLOCK / 4 * kChunks, kPer = (kUnits + kThreads - 1) / kThreads;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int u = threadIdx.x + i * kThreads, quad = u / kChunks, chunk = u % kChunks;
+      if (u >= kUnits || quad * 4 + 3 < it.lo || quad * 4 >= it.hi) continue;
+      f32x4 x[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) x[c] = decode4(*reinterpret_cast<const uint32_t *>(codes + v_place<D>(quad, chunk * 8 + c)));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = quad * 4 + j;
+        if (t < it.lo || t >= it.hi) continue;
+        u32x4 out;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) out[w] = pack_bf16x2(x[2 * w][j] * scale, x[2 * w + 1][j] * scale);
+        *reinterpret_cast<u32x4 *>(rows + (it.row0 + t) * side.view.sL + chunk * 8) = out;
+      }
+    }
+  } else {
+    constexpr int kUnits = BLOCK * kChunks;
+    static_assert(kUnits % kThreads == 0, "whole rounds");
+#pragma unroll
+    for (int i = 0; i < kUnits / kThreads; ++i) {
+      const int u = threadIdx.x + i * kThreads, t = u / kChunks, chunk = u % kChunks;
+      if (t < it.lo || t >= it.hi) continue;
+      const uint32_t *at = reinterpret_cast<const uint32_t *>(codes + k_place<D>(t, chunk));
+      const f32x4 lo = decode4(at[0]), hi = decode4(at[1]);
+      *reinterpret_cast<u32x4 *>(rows + (it.row0 + t) * side.view.sL + chunk * 8) =
+          u32x4{pack_bf16x2(lo[0] * scale, lo[1] * scale), pack_bf16x2(lo[2] * scale, lo[3] * scale),
+                pack_bf16x2(hi[0] * scale, hi[1] * scale), pack_bf16x2(hi[2] * scale, hi[3] * scale)};
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------------------
+namespace {
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLeastFactor = 1.17549435e-38f;   // (a factor of zero would make NaN of a masked score)
+
+// The two A operands that 16 codes of a tile are.
+struct Operands {
+  bf16x8 part[2];
+};
+__device__ __forceinline__ Operands widen(u32x4 codes) {
+  Operands r;
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    bf16x2 x[4];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      x[2 * w] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * u + w], 1.0f, false);
+      x[2 * w + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * u + w], 1.0f, true);
+    }
+    r.part[u] = bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
+  }
+#else
+  r = Operands{};
+#endif
+  return r;
+}
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+// Scales of a block as the inner loop wants them.
+struct BlockScale {
+  float c;          // of K, with the soft-max scale, in log2 units
+  float log2_v;     // of V: the probabilities carry it, so that the accumulators need no scaling of their own ...
+  float inv_v;      // ... and their sum takes it off again
+  __device__ __forceinline__ BlockScale(const CacheAttnArgs &a, int64_t block_index) {
+    c = fmaxf(a.scale_log2 * a.k_scale[block_index], kLeastFactor);
+    const float v = a.v_scale[block_index];
+    log2_v = __builtin_amdgcn_logf(v);
+    inv_v = 1.0f / v;
+  }
+};
+
+// 32 rows (queries) of one wavefront: lane (h, r) holds row r's running maximum and its half of the denominator.
+template <int D>
+struct Rows {
+  static constexpr int T = D / 32;
+  bf16x8 q[T][2];
+  f32x16 acc[T];     // O^T: register 4 g + j is channel 32 t + 8 g + 4 h + j
+  float m, l;
+
+  __device__ __forceinline__ void init(const bf16 *row, int half) {
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) q[t][u] = *reinterpret_cast<const bf16x8 *>(row + 32 * t + 16 * half + 8 * u);
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+    m = -__builtin_inff();
+    l = 0.f;
+  }
+
+  // 32 keys, of which the first `left` (> 0) exist; k(t), v(t): 16 codes of the lane in tile t
+  template <typename K, typename V>
+  __device__ __forceinline__ void attend(const K &k, const V &v, const BlockScale &bs, int left, int half) {
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const Operands kk = widen(k(t));
+      s = mfma(kk.part[0], q[t][0], s);
+      s = mfma(kk.part[1], q[t][1], s);
+    }
+    if (left < 32) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (8 * (i / 4) + 4 * half + i % 4 >= left) s[i] = -__builtin_inff();
+    }
+    float top = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    const float m_new = fmaxf(m, max_of_halves(top) * bs.c);
+    const float down = bs.log2_v - m_new;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = fast_exp2(__builtin_fmaf(s[i], bs.c, down));
+      sum += s[i];
+    }
+    if (__ballot(m_new != m)) {
+      const float shrink = fast_exp2(m - m_new);
+      l *= shrink;
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[t][i] *= shrink;
+      m = m_new;
+    }
+    l = __builtin_fmaf(sum, bs.inv_v, l);
+    bf16x8 p[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const u32x4 x = {pack_bf16x2(s[8 * u], s[8 * u + 1]), pack_bf16x2(s[8 * u + 2], s[8 * u + 3]),
+                       pack_bf16x2(s[8 * u + 4], s[8 * u + 5]), pack_bf16x2(s[8 * u + 6], s[8 * u + 7])};
+      p[u] = __builtin_bit_cast(bf16x8, x);
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      u32x4 codes = v(t);
+      if (left < 32) {       // what lies behind the last token may be a NaN
+#pragma unroll
+        for (int g = 0; g < 4; ++g) codes[g] &= bytes_within(8 * g + 4 * half, 0, left);
+      }
+      const Operands vv = widen(codes);
+      acc[t] = mfma(vv.part[0], p[0], acc[t]);
+      acc[t] = mfma(vv.part[1], p[1], acc[t]);
+    }
+  }
+};
+
+// Where a row of a unit (sequence, key head, block of queries, row tile) lies: rows of a block of queries go through the
+// query heads that share the key head, and through the block's tokens in each.
+struct Unit {
+  int slab, b, h_kv, qb, tile, tokens, rows;   // rows: of this tile that exist (<= 0: none)
+  __device__ __forceinline__ Unit(const CacheAttnArgs &a, int64_t unit) {
+    tile = (int)(unit % a.tiles);
+    const int64_t x = unit / a.tiles;
+    qb = (int)(x % a.n_qblocks);
+    slab = (int)(x / a.n_qblocks);
+    b = slab / a.H_kv;
+    h_kv = slab - b * a.H_kv;
+    tokens = min(a.block, a.L - qb * a.block);
+    rows = min(tokens * a.group - tile * a.tile_rows, a.tile_rows);
+  }
+  // head and token of row r of the tile
+  __device__ __forceinline__ void place(const CacheAttnArgs &a, int r, int &head, int &token) const {
+    const int x = tile * a.tile_rows + r, g = x / tokens;
+    head = h_kv * a.group + g;
+    token = qb * a.block + x - g * tokens;
+  }
+};
+
+// The blocks that a unit's split walks: positions [at, end) of the row's list, or of all blocks.
+struct Walk {
+  const int32_t *list;
+  int at, end, length, n_blocks;
+  __device__ __forceinline__ Walk(const CacheAttnArgs &a, const Unit &u, int split) {
+    length = (int)min((int64_t)max(a.length[u.b], 0), (int64_t)a.max_blocks * a.block);
+    n_blocks = (length + a.block - 1) / a.block;
+    int n = n_blocks;
+    list = nullptr;
+    if (a.row_ptr) {
+      const int room = a.n_qblocks * a.max_blocks;
+      const int32_t *ptr = a.row_ptr + (int64_t)u.slab * (a.n_qblocks + 1) + u.qb;
+      const int first = min(max(ptr[0], 0), room), last = min(max(ptr[1], first), room);
+      list = a.col_idx + (int64_t)u.slab * room + first;
+      n = min(last - first, a.max_blocks);      // (distinct blocks)
+    }
+    const int share = max((n + a.splits - 1) / a.splits, 1);
+    at = (int)min((int64_t)split * share, (int64_t)n);
+    end = min(at + share, n);
+  }
+  // block at a position; negative where the list names none that the sequence has
+  __device__ __forceinline__ int block(int position) const {
+    const int j = list ? list[position] : position;
+    return j >= 0 && j < n_blocks ? j : -1;
+  }
+};
+
+// The result of 32 rows: a row of o and lse, or of the split's partial sums.
+template <int D>
+__device__ __forceinline__ void put_rows(const CacheAttnArgs &a, const Unit &u, int64_t unit, int split, int row, int half,
+                                         const f32x16 (&acc)[D / 32], float m, float l) {
+  if (row >= u.rows) return;
+  const bool nothing = l == 0.f && m == -__builtin_inff();
+  if (a.splits > 1) {
+    const int64_t at = (unit * a.splits + split) * a.rows_kept + row;
+    float *ml = a.partial + (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles * a.splits * a.rows_kept * D + at * 2;
+    if (half == 0) {
+      ml[0] = m;
+      ml[1] = l;
+    }
+    if (nothing) return;
+    float *to = a.partial + at * D + 4 * half;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4 *>(to + 32 * t + 8 * g) = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+    return;
+  }
+  int head, token;
+  u.place(a, row, head, token);
+  const float f = nothing ? 0.f : 1.0f / l;
+  bf16 *to = reinterpret_cast<bf16 *>(a.o) + u.b * a.ov.sB + head * a.ov.sH + token * a.ov.sL + 4 * half;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<uint2 *>(to + 32 * t + 8 * g) = uint2{pack_bf16x2(acc[t][4 * g] * f, acc[t][4 * g + 1] * f),
+                                                             pack_bf16x2(acc[t][4 * g + 2] * f, acc[t][4 * g + 3] * f)};
+  if (half == 0) a.lse[((int64_t)u.b * a.H + head) * a.L + token] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+}  // namespace
+
+// Few rows (a token-by-token step): all of a tile's 32 rows in every wavefront, the keys shared out among the four.  What
+// bounds it is the cache's bytes; a wavefront has the next 32 keys' 2 * 32 * D bytes in flight while it works on these.
+template <int D, int BLOCK>
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(const CacheAttnArgs a) {
+  constexpr int T = D / 32, kGroups = BLOCK / 32, kWaves = kThreads / 64, kPitch = D + 4;
+  __shared__ float wave_m[kWaves][32], wave_l[kWaves][32];
+  __shared__ __align__(16) float half_acc[kWaves / 2][32 * kPitch];
+  const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
+  const int item = xcd_contiguous_work(blockIdx.x, (int)(units * a.splits));
+  if (item < 0) return;
+  const int64_t unit = item / a.splits;
+  const int split = item - (int)unit * a.splits;
+  const Unit u(a, unit);
+  if (u.rows <= 0) return;
+  const Walk walk(a, u, split);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, row = lane & 31;
+
+  Rows<D> rows;
+  {
+    int head, token;
+    u.place(a, min(row, u.rows - 1), head, token);
+    rows.init(reinterpret_cast<const bf16 *>(a.q) + u.b * a.qv.sB + head * a.qv.sH + token * a.qv.sL, half);
+  }
+  const int64_t block0 = (int64_t)u.slab * a.max_blocks;
+  const int end = walk.end * kGroups;
+  // groups of 32 keys, from `x` on, that exist
+  auto next = [&](int x, int &j) {
+    for (; x < end; x += kWaves) {
+      j = __builtin_amdgcn_readfirstlane(walk.block(x / kGroups));
+      if (j >= 0 && j * BLOCK + x % kGroups * 32 < walk.length) break;
+    }
+    return x;
+  };
+  struct Codes {
+    u32x4 k[T], v[T];
+  };
+  auto fetch = [&](int x, int j, Codes &c) {
+    const int64_t at = (block0 + j) * (BLOCK * D) + x % kGroups * (32 * D) + lane * 16;
+#pragma unroll
+    for (int t = 0; t < T; ++t) c.k[t] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(a.k) + at + t * 1024);
+#pragma unroll
+    for (int t = 0; t < T; ++t) c.v[t] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(a.v) + at + t * 1024);
+  };
+  Codes now, coming;
+  int j = 0, x = next(walk.at * kGroups + wave, j);
+  if (x < end) fetch(x, j, now);
+  while (x < end) {
+    int j_next = 0;
+    const int x_next = next(x + kWaves, j_next);
+    if (x_next < end) fetch(x_next, j_next, coming);
+    const BlockScale bs(a, block0 + j);
+    rows.attend([&](int t) { return now.k[t]; }, [&](int t) { return now.v[t]; }, bs,
+                walk.length - (j * BLOCK + x % kGroups * 32), half);
+    now = coming;
+    x = x_next;
+    j = j_next;
+  }
+
+  // the four wavefronts' parts of each row into one
+  rows.l += swap_halves(rows.l);
+  if (half == 0) {
+    wave_m[wave][row] = rows.m;
+    wave_l[wave][row] = rows.l;
+  }
+  __syncthreads();
+  float m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, wave_m[w][row]);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float mw = wave_m[w][row], lw = wave_l[w][row];
+    if (!(mw == -__builtin_inff() && lw == 0.f)) l = __builtin_fmaf(lw, fast_exp2(mw - m), l);
+  }
+  const float f = rows.m == -__builtin_inff() && rows.l == 0.f ? 0.f : fast_exp2(rows.m - m);
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) rows.acc[t][i] *= f;
+#pragma unroll
+  for (int step = kWaves / 2; step > 0; step /= 2) {
+    if (wave >= step && wave < 2 * step && row < u.rows) {
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4 *>(&half_acc[wave - step][row * kPitch + 32 * t + 8 * g + 4 * half]) =
+              f32x4{rows.acc[t][4 * g], rows.acc[t][4 * g + 1], rows.acc[t][4 * g + 2], rows.acc[t][4 * g + 3]};
+    }
+    __syncthreads();
+    if (wave < step && row < u.rows) {
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 other = *reinterpret_cast<const f32x4 *>(&half_acc[wave][row * kPitch + 32 * t + 8 * g + 4 * half]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) rows.acc[t][4 * g + i] += other[i];
+        }
+    }
+    __syncthreads();
+  }
+  if (wave == 0) put_rows<D>(a, u, unit, split, row, half, rows.acc, m, l);
+}
+
+// Many rows: four wavefronts of 32 rows each walk the listed blocks together; a block's codes are copied to LDS one
+// block ahead (two buffers), every wavefront widens what it reads.
+template <int D, int BLOCK>
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_tile_kernel(const CacheAttnArgs a) {
+  constexpr int kBytes = BLOCK * D, kGroups = BLOCK / 32, kWaves = kThreads / 64, kCopies = kBytes / 1024 / kWaves;
+  __shared__ __align__(16) char stage[2][2][kBytes];
+  const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
+  const int item = xcd_contiguous_work(blockIdx.x, (int)(units * a.splits));
+  if (item < 0) return;
+  const int64_t unit = item / a.splits;
+  const int split = item - (int)unit * a.splits;
+  const Unit u(a, unit);
+  if (u.rows <= 0) return;
+  const Walk walk(a, u, split);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int row = wave * 32 + (lane & 31);
+
+  Rows<D> rows;
+  {
+    int head, token;
+    u.place(a, min(row, u.rows - 1), head, token);
+    rows.init(reinterpret_cast<const bf16 *>(a.q) + u.b * a.qv.sB + head * a.qv.sH + token * a.qv.sL, half);
+  }
+  const int64_t block0 = (int64_t)u.slab * a.max_blocks;
+  auto next = [&](int x, int &j) {
+    for (; x < walk.end; ++x) {
+      j = __builtin_amdgcn_readfirstlane(walk.block(x));
+      if (j >= 0) break;
+    }
+    return x;
+  };
+  const uint32_t lane_off = (uint32_t)(wave * kCopies * 1024 + lane * 16);
+  auto copy = [&](int j, int buffer) {
+    const char *k = reinterpret_cast<const char *>(a.k) + (block0 + j) * kBytes;
+    const char *v = reinterpret_cast<const char *>(a.v) + (block0 + j) * kBytes;
+    const uint32_t to = ASA_LDS_ADDR_OF(stage) + buffer * (2 * kBytes) + wave * kCopies * 1024;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      lds_dma16_sv(k, lane_off + i * 1024, to + i * 1024);
+      lds_dma16_sv(v, lane_off + i * 1024, to + kBytes + i * 1024);
+    }
+  };
+  int j = 0, x = next(walk.at, j), buffer = 0;
+  if (x < walk.end) copy(j, 0);
+  while (x < walk.end) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#endif
+    __syncthreads();      // the block is there, and nobody reads the other buffer any more
+    int j_next = 0;
+    const int x_next = next(x + 1, j_next);
+    if (x_next < walk.end) copy(j_next, buffer ^ 1);
+    const BlockScale bs(a, block0 + j);
+    const int left = walk.length - j * BLOCK;
+    if (wave * 32 < u.rows) {
+#pragma unroll 1
+      for (int g = 0; g < kGroups; ++g) {
+        if (g * 32 >= left) break;
+        const char *k = &stage[buffer][0][g * 32 * D + lane * 16], *v = &stage[buffer][1][g * 32 * D + lane * 16];
+        rows.attend([&](int t) { return *reinterpret_cast<const u32x4 *>(k + t * 1024); },
+                    [&](int t) { return *reinterpret_cast<const u32x4 *>(v + t * 1024); }, bs, left - g * 32, half);
+      }
+    }
+    buffer ^= 1;
+    x = x_next;
+    j = j_next;
+  }
+  rows.l += swap_halves(rows.l);
+  put_rows<D>(a, u, unit, split, row, half, rows.acc, rows.m, rows.l);
+}
+
+// Joins the splits' parts of each row: D / 4 lanes a row.
+template <int D>
+__global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(const CacheAttnArgs a) {
+  constexpr int kLanes = D / 4;
+  const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
+  const int64_t r = (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
+  const int sub = threadIdx.x % kLanes;
+  if (r >= units * a.rows_kept) return;
+  const int64_t unit = r / a.rows_kept;
+  const int row = (int)(r - unit * a.rows_kept);
+  const Unit u(a, unit);
+  if (row >= u.rows) return;
+  const int64_t first = unit * a.splits * a.rows_kept + row;
+  const float *ml = a.partial + units * a.splits * a.rows_kept * D;
+  float m = -__builtin_inff();
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[(first + (int64_t)s * a.rows_kept) * 2]);
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; ++s) {
+    const int64_t at = first + (int64_t)s * a.rows_kept;
+    const float ms = ml[at * 2], ls = ml[at * 2 + 1];
+    if (ms == -__builtin_inff() && ls == 0.f) continue;
+    const float f = fast_exp2(ms - m);
+    const f32x4 part = *reinterpret_cast<const f32x4 *>(a.partial + at * D + sub * 4);
+    l = __builtin_fmaf(ls, f, l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(part[i], f, o[i]);
+  }
+  int head, token;
+  u.place(a, row, head, token);
+  const float f = l == 0.f && m == -__builtin_inff() ? 0.f : 1.0f / l;
+  bf16 *to = reinterpret_cast<bf16 *>(a.o) + u.b * a.ov.sB + head * a.ov.sH + token * a.ov.sL + sub * 4;
+  *reinterpret_cast<uint2 *>(to) = uint2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
+  if (sub == 0) a.lse[((int64_t)u.b * a.H + head) * a.L + token] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------
+int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, CacheAttnPlan *plan) {
+  const int group = pb.H / H_kv;
+  const int64_t rows = (int64_t)(pb.L < pb.block ? pb.L : pb.block) * group;   // of one list
+  plan->n_qblocks = pb.Nb;
+  plan->tile_rows = rows <= 32 ? 32 : 128;
+  plan->tiles = (int)((rows + plan->tile_rows - 1) / plan->tile_rows);
+  plan->rows_kept = (int)(rows < plan->tile_rows ? rows : plan->tile_rows);
+  plan->units = (int64_t)pb.B * H_kv * pb.Nb * plan->tiles;
+  const int64_t wanted = plan->tile_rows == 32 ? 2048 : 512;
+  int64_t splits = wanted / plan->units;
+  const int64_t most = ((int64_t)max_blocks * pb.block + 255) / 256;
+  if (splits > most) splits = most;
+  plan->splits = splits < 1 ? 1 : (int)splits;
+  if ((int64_t)pb.Nb * max_blocks >= ((int64_t)1 << 31)) return ASA_ERR_UNSUPPORTED;
+  return plan->units * plan->splits < ((int64_t)1 << 31) - 64 ? ASA_OK : ASA_ERR_UNSUPPORTED;
+}
+
+size_t cache_attn_workspace_bytes(const Problem &pb, const CacheAttnPlan &plan) {
+  if (plan.splits == 1) return 0;
+  return (size_t)plan.units * plan.splits * plan.rows_kept * (pb.d + 2) * sizeof(float);
+}
+
+template <int D, int BLOCK>
+static hipError_t launch_cache_attn_as(const CacheAttnArgs &a, hipStream_t st) {
+  const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
+  const int grid = xcd_grid((int)(units * a.splits));
+  if (a.tile_rows == 32) cache_attn_rows_kernel<D, BLOCK><<<grid, kThreads, 0, st>>>(a);
+  else cache_attn_tile_kernel<D, BLOCK><<<grid, kThreads, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int per = kThreads / (D / 4);
+  cache_attn_join_kernel<D><<<(int)((units * a.rows_kept + per - 1) / per), kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_cache_attn(const CacheAttnArgs &a, int D, hipStream_t st) {
+  if (D == 128) return a.block == 128 ? launch_cache_attn_as<128, 128>(a, st) : launch_cache_attn_as<128, 64>(a, st);
+  return a.block == 128 ? launch_cache_attn_as<64, 128>(a, st) : launch_cache_attn_as<64, 64>(a, st);
+}
+
+template <int D, int BLOCK>
+static hipError_t launch_cache_as(const CacheArgs &a, bool write, hipStream_t st) {
+  const int grid = a.reached * a.H * a.B * a.n_sides;
+  if (write) cache_write_kernel<D, BLOCK><<<grid, kThreads, 0, st>>>(a);
+  else cache_read_kernel<D, BLOCK><<<grid, kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+static hipError_t launch_cache(const CacheArgs &a, int D, int block, bool write, hipStream_t st) {
+  if (D == 128) return block == 128 ? launch_cache_as<128, 128>(a, write, st) : launch_cache_as<128, 64>(a, write, st);
+  return block == 128 ? launch_cache_as<64, 128>(a, write, st) : launch_cache_as<64, 64>(a, write, st);
+}
+hipError_t launch_cache_write(const CacheArgs &a, int D, int block, hipStream_t st) { return launch_cache(a, D, block, true, st); }
+hipError_t launch_cache_read(const CacheArgs &a, int D, int block, hipStream_t st) { return launch_cache(a, D, block, false, st); }
+
+}  // namespace asa
