@@ -298,6 +298,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(const CacheArgs a)
 // ---------------------------------------------------------------------------------------
 namespace {
 
+constexpr int kMaxSplits = kThreads, kFewSplits = 4;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLeastFactor = 1.17549435e-38f;   // (a factor of zero would make NaN of a masked score)
 
@@ -614,11 +615,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(const Cach
   if (wave == 0) put_rows<D>(a, u, unit, split, row, half, rows.acc, m, l);
 }
 
-// Many rows: four wavefronts of 32 rows each walk the listed blocks together; a block's codes are copied to LDS one
-// block ahead (two buffers), every wavefront widens what it reads.
-template <int D, int BLOCK>
-__global__ __launch_bounds__(kThreads, 2) void cache_attn_tile_kernel(const CacheAttnArgs a) {
-  constexpr int kBytes = BLOCK * D, kGroups = BLOCK / 32, kWaves = kThreads / 64, kCopies = kBytes / 1024 / kWaves;
+// Many rows: two or four wavefronts of 32 rows each walk the listed blocks together; a block's codes are copied to LDS
+// one block ahead (two buffers), every wavefront widens what it reads.
+template <int D, int BLOCK, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_tile_kernel(const CacheAttnArgs a) {
+  constexpr int kBytes = BLOCK * D, kGroups = BLOCK / 32, kCopies = kBytes / 1024 / WAVES;
   __shared__ __align__(16) char stage[2][2][kBytes];
   const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
   const int item = xcd_contiguous_work(blockIdx.x, (int)(units * a.splits));
@@ -685,33 +686,73 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_tile_kernel(const Cach
   put_rows<D>(a, u, unit, split, row, half, rows.acc, rows.m, rows.l);
 }
 
-// Joins the splits' parts of each row: D / 4 lanes a row.
-template <int D>
+// Joins the splits' parts of each row.  kMaxSplits / few: D / 4 lanes take a row, `GROUPS` of them its splits in turn,
+// joined through LDS: a row that was cut into 170 parts is one workgroup's work (one lane group alone takes 110 us for it,
+// a load's latency for each part), many rows of a few parts are several to a workgroup.
+template <int D, int GROUPS>
 __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(const CacheAttnArgs a) {
-  constexpr int kLanes = D / 4;
+  constexpr int kLanes = D / 4, kRows = kThreads / kLanes / GROUPS;
+  __shared__ float factor[GROUPS > 1 ? kMaxSplits : 1], wave_m[kThreads / 64], wave_l[kThreads / 64];
+  __shared__ __align__(16) f32x4 part[GROUPS > 1 ? GROUPS : 1][kLanes];
   const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
-  const int64_t r = (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
-  const int sub = threadIdx.x % kLanes;
+  const int64_t r = (int64_t)blockIdx.x * kRows + (GROUPS > 1 ? 0 : threadIdx.x / kLanes);
+  const int sub = threadIdx.x % kLanes, group = GROUPS > 1 ? threadIdx.x / kLanes : 0;
   if (r >= units * a.rows_kept) return;
   const int64_t unit = r / a.rows_kept;
   const int row = (int)(r - unit * a.rows_kept);
   const Unit u(a, unit);
   if (row >= u.rows) return;
   const int64_t first = unit * a.splits * a.rows_kept + row;
-  const float *ml = a.partial + units * a.splits * a.rows_kept * D;
-  float m = -__builtin_inff();
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[(first + (int64_t)s * a.rows_kept) * 2]);
-  float l = 0.f;
+  const f32x2 *ml = reinterpret_cast<const f32x2 *>(a.partial + units * a.splits * a.rows_kept * D);
+  float m = -__builtin_inff(), l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const int64_t at = first + (int64_t)s * a.rows_kept;
-    const float ms = ml[at * 2], ls = ml[at * 2 + 1];
-    if (ms == -__builtin_inff() && ls == 0.f) continue;
-    const float f = fast_exp2(ms - m);
-    const f32x4 part = *reinterpret_cast<const f32x4 *>(a.partial + at * D + sub * 4);
-    l = __builtin_fmaf(ls, f, l);
+  if constexpr (GROUPS > 1) {
+    f32x2 mine = {-__builtin_inff(), 0.f};
+    if ((int)threadIdx.x < a.splits) mine = ml[first + (int64_t)threadIdx.x * a.rows_kept];
+    m = mine[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(part[i], f, o[i]);
+    for (int s = 32; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
+    if (threadIdx.x % 64 == 0) wave_m[threadIdx.x / 64] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) m = fmaxf(m, wave_m[w]);
+    // (a part without a key has left its sums unwritten: factor 0 and no read)
+    const bool nothing = mine[0] == -__builtin_inff() && mine[1] == 0.f;
+    const float f = nothing ? 0.f : fast_exp2(mine[0] - m);
+    if ((int)threadIdx.x < kMaxSplits) factor[threadIdx.x] = f;
+    l = nothing ? 0.f : mine[1] * f;
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) l += __shfl_xor(l, s, 64);
+    if (threadIdx.x % 64 == 0) wave_l[threadIdx.x / 64] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) l += wave_l[w];
+#pragma unroll 4
+    for (int s = group; s < a.splits; s += GROUPS) {
+      const float fs = factor[s];
+      if (fs == 0.f) continue;
+      const f32x4 p = *reinterpret_cast<const f32x4 *>(a.partial + (first + (int64_t)s * a.rows_kept) * D + sub * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(p[i], fs, o[i]);
+    }
+    part[group][sub] = o;
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) o += part[g][sub];
+  } else {
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[first + (int64_t)s * a.rows_kept][0]);
+    for (int s = 0; s < a.splits; ++s) {
+      const int64_t at = first + (int64_t)s * a.rows_kept;
+      const f32x2 mine = ml[at];
+      if (mine[0] == -__builtin_inff() && mine[1] == 0.f) continue;
+      const float f = fast_exp2(mine[0] - m);
+      const f32x4 p = *reinterpret_cast<const f32x4 *>(a.partial + at * D + sub * 4);
+      l = __builtin_fmaf(mine[1], f, l);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(p[i], f, o[i]);
+    }
   }
   int head, token;
   u.place(a, row, head, token);
@@ -728,7 +769,7 @@ int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, CacheAttnPlan *
   const int group = pb.H / H_kv;
   const int64_t rows = (int64_t)(pb.L < pb.block ? pb.L : pb.block) * group;   // of one list
   plan->n_qblocks = pb.Nb;
-  plan->tile_rows = rows <= 32 ? 32 : 128;
+  plan->tile_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   plan->tiles = (int)((rows + plan->tile_rows - 1) / plan->tile_rows);
   plan->rows_kept = (int)(rows < plan->tile_rows ? rows : plan->tile_rows);
   plan->units = (int64_t)pb.B * H_kv * pb.Nb * plan->tiles;
@@ -736,6 +777,7 @@ int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, CacheAttnPlan *
   int64_t splits = wanted / plan->units;
   const int64_t most = ((int64_t)max_blocks * pb.block + 255) / 256;
   if (splits > most) splits = most;
+  if (splits > kMaxSplits) splits = kMaxSplits;
   plan->splits = splits < 1 ? 1 : (int)splits;
   if ((int64_t)pb.Nb * max_blocks >= ((int64_t)1 << 31)) return ASA_ERR_UNSUPPORTED;
   return plan->units * plan->splits < ((int64_t)1 << 31) - 64 ? ASA_OK : ASA_ERR_UNSUPPORTED;
@@ -751,11 +793,14 @@ static hipError_t launch_cache_attn_as(const CacheAttnArgs &a, hipStream_t st) {
   const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
   const int grid = xcd_grid((int)(units * a.splits));
   if (a.tile_rows == 32) cache_attn_rows_kernel<D, BLOCK><<<grid, kThreads, 0, st>>>(a);
-  else cache_attn_tile_kernel<D, BLOCK><<<grid, kThreads, 0, st>>>(a);
+  else if (a.tile_rows == 64) cache_attn_tile_kernel<D, BLOCK, 2><<<grid, 128, 0, st>>>(a);
+  else cache_attn_tile_kernel<D, BLOCK, 4><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  const int per = kThreads / (D / 4);
-  cache_attn_join_kernel<D><<<(int)((units * a.rows_kept + per - 1) / per), kThreads, 0, st>>>(a);
+  constexpr int kGroups = kThreads / (D / 4);
+  const int64_t rows = units * a.rows_kept;
+  if (a.splits > kFewSplits) cache_attn_join_kernel<D, kGroups><<<(int)rows, kThreads, 0, st>>>(a);
+  else cache_attn_join_kernel<D, 1><<<(int)((rows + kGroups - 1) / kGroups), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_cache_attn(const CacheAttnArgs &a, int D, hipStream_t st) {

@@ -267,25 +267,36 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(const NormAr
   }
 }
 
-// out[ch] = sum over the workgroups' partial rows: 32 channels of one of the four sums for each workgroup, 32 threads a
-// channel, each every 32nd row in ascending order.
+// out[ch] = sum over the workgroups' partial rows: 32 channels of one of the four sums for each workgroup, a quarter
+// row to 8 threads, 128 rows at a time, then through LDS; always in the same order.
 __global__ __launch_bounds__(1024) void norm_sums_kernel(const NormArgs a, int D) {
   const NormSide &side = a.side[blockIdx.y];
   const int which = blockIdx.z;
   float *out = which ? side.db : side.dw;
   if (!out) return;
-  __shared__ float part[32][33];
-  const int c = threadIdx.x % 32, s = threadIdx.x / 32, ch = blockIdx.x * 32 + c;
-  const float *p = side.partial + (int64_t)which * side.groups * D + ch;
-  float total = 0.f;
-  for (int g = s; g < side.groups; g += 32) total += p[(int64_t)g * D];
-  part[s][c] = total;
-  __syncthreads();
-  if (s == 0) {
-    float x = 0.f;
+  __shared__ float part[128][33];
+  const int c = threadIdx.x % 8 * 4, s = threadIdx.x / 8;
+  const float *p = side.partial + (int64_t)which * side.groups * D + blockIdx.x * 32 + c;
+  f32x4 total = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 32; ++i) x += part[i][c];
-    out[ch] = x;
+  for (int i = 0; i < kMaxGroups / 128; ++i) {      // (loads without a branch: all of them are in flight at once)
+    const int g = s + i * 128;
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(p + (int64_t)min(g, side.groups - 1) * D);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) total[j] += g < side.groups ? x[j] : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) part[s][c + j] = total[j];
+  for (int half = 64; half >= 32; half /= 2) {
+    __syncthreads();
+    for (int e = threadIdx.x; e < half * 32; e += 1024) part[e / 32][e % 32] += part[e / 32 + half][e % 32];
+  }
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sum += part[i][threadIdx.x];
+    out[blockIdx.x * 32 + threadIdx.x] = sum;
   }
 }
 
