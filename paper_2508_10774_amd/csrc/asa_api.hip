@@ -704,7 +704,7 @@ int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v,
   return finish(launch_cache_read(a, p->d, p->block, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
-static int check_cache_attn(const asa_params *p, const asa_kv_cache *c, Problem *pb, CacheAttnPlan *plan) {
+static int check_cache_attn(const asa_params *p, const asa_kv_cache *c, bool lists, Problem *pb, CacheAttnPlan *plan) {
   if (!p || !c) return ASA_ERR_INVALID_ARG;
   int rc = resolve_shape(p, p->H, p->block, pb);
   if (rc != ASA_OK) return rc;
@@ -713,21 +713,26 @@ static int check_cache_attn(const asa_params *p, const asa_kv_cache *c, Problem 
   if (!view_from(p->q_stride, *pb, &pb->q) || !view_from(p->o_stride, *pb, &pb->o)) return ASA_ERR_INVALID_ARG;
   if (c->H_kv < 1 || c->max_blocks < 1 || pb->H % c->H_kv) return ASA_ERR_INVALID_ARG;
   if (c->max_blocks > 65536) return ASA_ERR_UNSUPPORTED;
-  return plan_cache_attn(*pb, c->H_kv, c->max_blocks, plan);
+  return plan_cache_attn(*pb, c->H_kv, c->max_blocks, lists, plan);
 }
 
 size_t asa_attn_cache_workspace_bytes(const asa_params *p, const asa_kv_cache *c) {
   Problem pb;
   CacheAttnPlan plan;
-  if (check_cache_attn(p, c, &pb, &plan) != ASA_OK) return 0;
-  return round256(cache_attn_workspace_bytes(pb, plan));
+  size_t most = 0;      // enough with lists and without
+  for (const bool lists : {false, true}) {
+    if (check_cache_attn(p, c, lists, &pb, &plan) != ASA_OK) return 0;
+    const size_t bytes = round256(cache_attn_workspace_bytes(pb, plan));
+    if (bytes > most) most = bytes;
+  }
+  return most;
 }
 
 int asa_attn_cache(const asa_params *p, const asa_kv_cache *c, const int32_t *length, const void *q, const int32_t *row_ptr,
                    const int32_t *col_idx, void *o, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
   Problem pb;
   CacheAttnPlan plan;
-  int rc = check_cache_attn(p, c, &pb, &plan);
+  int rc = check_cache_attn(p, c, row_ptr != nullptr, &pb, &plan);
   if (rc != ASA_OK) return rc;
   rc = check_cache(p, c, true, true);
   if (rc != ASA_OK) return rc;

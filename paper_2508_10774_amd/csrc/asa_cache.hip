@@ -298,7 +298,9 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(const CacheArgs a)
 // ---------------------------------------------------------------------------------------
 namespace {
 
-constexpr int kMaxSplits = kThreads, kFewSplits = 4;
+constexpr int kMaxSplits = kThreads;
+constexpr int64_t kMostItems = ((int64_t)1 << 31) - 64;   // workgroups of a launch
+constexpr int64_t kFewRows = 4096;   // up to here the join has a workgroup for each row
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLeastFactor = 1.17549435e-38f;   // (a factor of zero would make NaN of a masked score)
 
@@ -332,16 +334,29 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
 #endif
 }
 
+// A word that is the same for the whole wavefront and that the kernel does not write: read through the scalar cache, also
+// behind written-out loads, whose memory clobber would make a vector load (and a wait for all copies in flight) of it.
+template <typename T>
+__device__ __forceinline__ T uniform_read(const T *p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint64_t s = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x) |
+                     ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32);
+  return *reinterpret_cast<const __attribute__((address_space(4))) T *>(s);
+#else
+  return *p;
+#endif
+}
+
 // Scales of a block as the inner loop wants them.
 struct BlockScale {
   float c;          // of K, with the soft-max scale, in log2 units
   float log2_v;     // of V: the probabilities carry it, so that the accumulators need no scaling of their own ...
   float inv_v;      // ... and their sum takes it off again
-  __device__ __forceinline__ BlockScale(const CacheAttnArgs &a, int64_t block_index) {
-    c = fmaxf(a.scale_log2 * a.k_scale[block_index], kLeastFactor);
-    const float v = a.v_scale[block_index];
+  __device__ __forceinline__ BlockScale(const CacheAttnArgs &a, float k, float v) {
+    c = fmaxf(a.scale_log2 * k, kLeastFactor);
     log2_v = __builtin_amdgcn_logf(v);
-    inv_v = 1.0f / v;
+    inv_v = __builtin_amdgcn_rcpf(v);     // (exact for a power of two, else within a last bit)
   }
 };
 
@@ -366,34 +381,35 @@ struct Rows {
     l = 0.f;
   }
 
-  // 32 keys, of which the first `left` (> 0) exist; k(t), v(t): 16 codes of the lane in tile t
-  template <typename K, typename V>
+  // NG groups of 32 keys (MASKED: of which the first `left` > 0 keys exist); k(n, t), v(n, t): 16 codes of the lane in tile t
+  template <int NG, bool MASKED, typename K, typename V>
   __device__ __forceinline__ void attend(const K &k, const V &v, const BlockScale &bs, int left, int half) {
-    f32x16 s;
+    f32x16 s[NG];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int n = 0; n < NG; ++n) {
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const Operands kk = widen(k(t));
-      s = mfma(kk.part[0], q[t][0], s);
-      s = mfma(kk.part[1], q[t][1], s);
+      for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const Operands kk = widen(k(n, t));
+        s[n] = mfma(kk.part[0], q[t][0], s[n]);
+        s[n] = mfma(kk.part[1], q[t][1], s[n]);
+      }
     }
-    if (left < 32) {
+    if (MASKED) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (8 * (i / 4) + 4 * half + i % 4 >= left) s[i] = -__builtin_inff();
+      for (int n = 0; n < NG; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * n + 8 * (i / 4) + 4 * half + i % 4 >= left) s[n][i] = -__builtin_inff();
     }
-    float top = s[0];
+    float top = s[0][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    for (int n = 0; n < NG; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
     const float m_new = fmaxf(m, max_of_halves(top) * bs.c);
     const float down = bs.log2_v - m_new;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = fast_exp2(__builtin_fmaf(s[i], bs.c, down));
-      sum += s[i];
-    }
     if (__ballot(m_new != m)) {
       const float shrink = fast_exp2(m - m_new);
       l *= shrink;
@@ -403,25 +419,34 @@ struct Rows {
         for (int i = 0; i < 16; ++i) acc[t][i] *= shrink;
       m = m_new;
     }
-    l = __builtin_fmaf(sum, bs.inv_v, l);
-    bf16x8 p[2];
+    float sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const u32x4 x = {pack_bf16x2(s[8 * u], s[8 * u + 1]), pack_bf16x2(s[8 * u + 2], s[8 * u + 3]),
-                       pack_bf16x2(s[8 * u + 4], s[8 * u + 5]), pack_bf16x2(s[8 * u + 6], s[8 * u + 7])};
-      p[u] = __builtin_bit_cast(bf16x8, x);
-    }
+    for (int n = 0; n < NG; ++n) {
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      u32x4 codes = v(t);
-      if (left < 32) {       // what lies behind the last token may be a NaN
-#pragma unroll
-        for (int g = 0; g < 4; ++g) codes[g] &= bytes_within(8 * g + 4 * half, 0, left);
+      for (int i = 0; i < 16; ++i) {
+        s[n][i] = fast_exp2(__builtin_fmaf(s[n][i], bs.c, down));
+        sum += s[n][i];
       }
-      const Operands vv = widen(codes);
-      acc[t] = mfma(vv.part[0], p[0], acc[t]);
-      acc[t] = mfma(vv.part[1], p[1], acc[t]);
+      bf16x8 p[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const u32x4 x = {pack_bf16x2(s[n][8 * u], s[n][8 * u + 1]), pack_bf16x2(s[n][8 * u + 2], s[n][8 * u + 3]),
+                         pack_bf16x2(s[n][8 * u + 4], s[n][8 * u + 5]), pack_bf16x2(s[n][8 * u + 6], s[n][8 * u + 7])};
+        p[u] = __builtin_bit_cast(bf16x8, x);
+      }
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        u32x4 codes = v(n, t);
+        if (MASKED) {       // what lies behind the last token may be a NaN
+#pragma unroll
+          for (int g = 0; g < 4; ++g) codes[g] &= bytes_within(32 * n + 8 * g + 4 * half, 0, left);
+        }
+        const Operands vv = widen(codes);
+        acc[t] = mfma(vv.part[0], p[0], acc[t]);
+        acc[t] = mfma(vv.part[1], p[1], acc[t]);
+      }
     }
+    l = __builtin_fmaf(sum, bs.inv_v, l);
   }
 };
 
@@ -469,9 +494,59 @@ struct Walk {
   }
   // block at a position; negative where the list names none that the sequence has
   __device__ __forceinline__ int block(int position) const {
-    const int j = list ? list[position] : position;
+    const int j = list ? uniform_read(list + position) : position;
     return j >= 0 && j < n_blocks ? j : -1;
   }
+};
+
+// Steps of KEYS keys along a walk, STRIDE apart: those that are full, one after the other; the one that the sequence ends
+// in (there is one at most) is kept for the end, so that the loop over the others need not mask.
+template <int BLOCK, int KEYS, int STRIDE>
+struct Steps {
+  static constexpr int kPerBlock = BLOCK / KEYS;
+  const Walk &walk;
+  const CacheAttnArgs &a;
+  int64_t block0;
+  int x, end, j;              // step, its block
+  float k_scale, v_scale;     // of the block, on their way while the step before is worked on
+  int last_x, last_j;
+  __device__ __forceinline__ Steps(const CacheAttnArgs &a_, const Walk &w, int64_t block0_, int first)
+      : walk(w), a(a_), block0(block0_), end(w.end * kPerBlock), j(0), k_scale(1.f), v_scale(1.f), last_x(-1), last_j(0) {
+    find(w.at * kPerBlock + first);
+  }
+  __device__ __forceinline__ bool any() const { return x < end; }
+  __device__ __forceinline__ void advance() { find(x + STRIDE); }
+  __device__ __forceinline__ void find(int from) {
+    for (x = from; x < end; x += STRIDE) {
+      j = __builtin_amdgcn_readfirstlane(walk.block(x / kPerBlock));
+      if (j < 0) continue;
+      const int left = walk.length - keys_before();
+      if (left >= KEYS) {
+        scales();
+        return;
+      }
+      if (left > 0) {
+        last_x = x;
+        last_j = j;
+      }
+    }
+  }
+  // the step that the sequence ends in becomes the current one
+  __device__ __forceinline__ bool to_last() {
+    if (last_x < 0) return false;
+    x = last_x;
+    j = last_j;
+    scales();
+    return true;
+  }
+  __device__ __forceinline__ void scales() {
+    k_scale = uniform_read(a.k_scale + block0 + j);
+    v_scale = uniform_read(a.v_scale + block0 + j);
+  }
+  __device__ __forceinline__ int keys_before() const { return j * BLOCK + x % kPerBlock * KEYS; }
+  // byte address of the step's codes, of K and of V
+  template <int D>
+  __device__ __forceinline__ int64_t codes() const { return (block0 + j) * (BLOCK * D) + x % kPerBlock * (KEYS * D); }
 };
 
 // The result of 32 rows: a row of o and lse, or of the split's partial sums.
@@ -515,7 +590,7 @@ __device__ __forceinline__ void put_rows(const CacheAttnArgs &a, const Unit &u, 
 // bounds it is the cache's bytes; a wavefront has the next 32 keys' 2 * 32 * D bytes in flight while it works on these.
 template <int D, int BLOCK>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(const CacheAttnArgs a) {
-  constexpr int T = D / 32, kGroups = BLOCK / 32, kWaves = kThreads / 64, kPitch = D + 4;
+  constexpr int T = D / 32, kWaves = kThreads / 64, kPitch = D + 4;
   __shared__ float wave_m[kWaves][32], wave_l[kWaves][32];
   __shared__ __align__(16) float half_acc[kWaves / 2][32 * kPitch];
   const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
@@ -534,39 +609,31 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(const Cach
     u.place(a, min(row, u.rows - 1), head, token);
     rows.init(reinterpret_cast<const bf16 *>(a.q) + u.b * a.qv.sB + head * a.qv.sH + token * a.qv.sL, half);
   }
-  const int64_t block0 = (int64_t)u.slab * a.max_blocks;
-  const int end = walk.end * kGroups;
-  // groups of 32 keys, from `x` on, that exist
-  auto next = [&](int x, int &j) {
-    for (; x < end; x += kWaves) {
-      j = __builtin_amdgcn_readfirstlane(walk.block(x / kGroups));
-      if (j >= 0 && j * BLOCK + x % kGroups * 32 < walk.length) break;
-    }
-    return x;
-  };
   struct Codes {
     u32x4 k[T], v[T];
   };
-  auto fetch = [&](int x, int j, Codes &c) {
-    const int64_t at = (block0 + j) * (BLOCK * D) + x % kGroups * (32 * D) + lane * 16;
+  auto fetch = [&](int64_t at, Codes &c) {
+    const char *k = reinterpret_cast<const char *>(a.k) + at + lane * 16, *v = reinterpret_cast<const char *>(a.v) + at + lane * 16;
 #pragma unroll
-    for (int t = 0; t < T; ++t) c.k[t] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(a.k) + at + t * 1024);
+    for (int t = 0; t < T; ++t) c.k[t] = *reinterpret_cast<const u32x4 *>(k + t * 1024);
 #pragma unroll
-    for (int t = 0; t < T; ++t) c.v[t] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(a.v) + at + t * 1024);
+    for (int t = 0; t < T; ++t) c.v[t] = *reinterpret_cast<const u32x4 *>(v + t * 1024);
   };
-  Codes now, coming;
-  int j = 0, x = next(walk.at * kGroups + wave, j);
-  if (x < end) fetch(x, j, now);
-  while (x < end) {
-    int j_next = 0;
-    const int x_next = next(x + kWaves, j_next);
-    if (x_next < end) fetch(x_next, j_next, coming);
-    const BlockScale bs(a, block0 + j);
-    rows.attend([&](int t) { return now.k[t]; }, [&](int t) { return now.v[t]; }, bs,
-                walk.length - (j * BLOCK + x % kGroups * 32), half);
+  Codes now, coming, after;
+  auto k_now = [&](int, int t) { return now.k[t]; };
+  auto v_now = [&](int, int t) { return now.v[t]; };
+  Steps<BLOCK, 32, kWaves> step(a, walk, (int64_t)u.slab * a.max_blocks, wave);
+  if (step.any()) fetch(step.template codes<D>(), now);
+  while (step.any()) {
+    const BlockScale bs(a, step.k_scale, step.v_scale);
+    step.advance();
+    if (step.any()) fetch(step.template codes<D>(), coming);
+    rows.template attend<1, false>(k_now, v_now, bs, 32, half);
     now = coming;
-    x = x_next;
-    j = j_next;
+  }
+  if (step.to_last()) {
+    fetch(step.template codes<D>(), now);
+    rows.template attend<1, true>(k_now, v_now, BlockScale(a, step.k_scale, step.v_scale), walk.length - step.keys_before(), half);
   }
 
   // the four wavefronts' parts of each row into one
@@ -615,11 +682,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(const Cach
   if (wave == 0) put_rows<D>(a, u, unit, split, row, half, rows.acc, m, l);
 }
 
-// Many rows: two or four wavefronts of 32 rows each walk the listed blocks together; a block's codes are copied to LDS
-// one block ahead (two buffers), every wavefront widens what it reads.
+// Many rows: two or four wavefronts of 32 rows each walk the listed blocks together, 64 keys at a time; the codes of the
+// next 64 are copied to LDS meanwhile (two buffers), every wavefront widens what it reads.
 template <int D, int BLOCK, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_tile_kernel(const CacheAttnArgs a) {
-  constexpr int kBytes = BLOCK * D, kGroups = BLOCK / 32, kCopies = kBytes / 1024 / WAVES;
+  constexpr int kKeys = 64, kBytes = kKeys * D, kCopies = kBytes / 1024 / WAVES;
   __shared__ __align__(16) char stage[2][2][kBytes];
   const int64_t units = (int64_t)a.B * a.H_kv * a.n_qblocks * a.tiles;
   const int item = xcd_contiguous_work(blockIdx.x, (int)(units * a.splits));
@@ -638,18 +705,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_tile_kernel(const Ca
     u.place(a, min(row, u.rows - 1), head, token);
     rows.init(reinterpret_cast<const bf16 *>(a.q) + u.b * a.qv.sB + head * a.qv.sH + token * a.qv.sL, half);
   }
-  const int64_t block0 = (int64_t)u.slab * a.max_blocks;
-  auto next = [&](int x, int &j) {
-    for (; x < walk.end; ++x) {
-      j = __builtin_amdgcn_readfirstlane(walk.block(x));
-      if (j >= 0) break;
-    }
-    return x;
-  };
   const uint32_t lane_off = (uint32_t)(wave * kCopies * 1024 + lane * 16);
-  auto copy = [&](int j, int buffer) {
-    const char *k = reinterpret_cast<const char *>(a.k) + (block0 + j) * kBytes;
-    const char *v = reinterpret_cast<const char *>(a.v) + (block0 + j) * kBytes;
+  auto copy = [&](int64_t at, int buffer) {
+    const char *k = reinterpret_cast<const char *>(a.k) + at, *v = reinterpret_cast<const char *>(a.v) + at;
     const uint32_t to = ASA_LDS_ADDR_OF(stage) + buffer * (2 * kBytes) + wave * kCopies * 1024;
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
@@ -657,38 +715,39 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_tile_kernel(const Ca
       lds_dma16_sv(v, lane_off + i * 1024, to + kBytes + i * 1024);
     }
   };
-  int j = 0, x = next(walk.at, j), buffer = 0;
-  if (x < walk.end) copy(j, 0);
-  while (x < walk.end) {
+  auto arrived = [&]() {      // my copies, then everybody's
 #if defined(__HIP_DEVICE_COMPILE__)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #endif
-    __syncthreads();      // the block is there, and nobody reads the other buffer any more
-    int j_next = 0;
-    const int x_next = next(x + 1, j_next);
-    if (x_next < walk.end) copy(j_next, buffer ^ 1);
-    const BlockScale bs(a, block0 + j);
-    const int left = walk.length - j * BLOCK;
-    if (wave * 32 < u.rows) {
-#pragma unroll 1
-      for (int g = 0; g < kGroups; ++g) {
-        if (g * 32 >= left) break;
-        const char *k = &stage[buffer][0][g * 32 * D + lane * 16], *v = &stage[buffer][1][g * 32 * D + lane * 16];
-        rows.attend([&](int t) { return *reinterpret_cast<const u32x4 *>(k + t * 1024); },
-                    [&](int t) { return *reinterpret_cast<const u32x4 *>(v + t * 1024); }, bs, left - g * 32, half);
-      }
-    }
+    __syncthreads();
+  };
+  const bool mine = wave * 32 < u.rows;
+  int buffer = 0;
+  auto k_now = [&](int n, int t) { return *reinterpret_cast<const u32x4 *>(&stage[buffer][0][lane * 16 + n * 32 * D + t * 1024]); };
+  auto v_now = [&](int n, int t) { return *reinterpret_cast<const u32x4 *>(&stage[buffer][1][lane * 16 + n * 32 * D + t * 1024]); };
+  Steps<BLOCK, kKeys, 1> step(a, walk, (int64_t)u.slab * a.max_blocks, 0);
+  if (step.any()) copy(step.template codes<D>(), 0);
+  while (step.any()) {
+    arrived();              // (nobody reads the other buffer any more, either)
+    const BlockScale bs(a, step.k_scale, step.v_scale);
+    step.advance();
+    if (step.any()) copy(step.template codes<D>(), buffer ^ 1);
+    if (mine) rows.template attend<2, false>(k_now, v_now, bs, kKeys, half);
     buffer ^= 1;
-    x = x_next;
-    j = j_next;
+  }
+  if (step.to_last()) {
+    copy(step.template codes<D>(), buffer);      // (this one was read before the last barrier)
+    arrived();
+    if (mine)
+      rows.template attend<2, true>(k_now, v_now, BlockScale(a, step.k_scale, step.v_scale), walk.length - step.keys_before(), half);
   }
   rows.l += swap_halves(rows.l);
   put_rows<D>(a, u, unit, split, row, half, rows.acc, rows.m, rows.l);
 }
 
-// Joins the splits' parts of each row.  kMaxSplits / few: D / 4 lanes take a row, `GROUPS` of them its splits in turn,
-// joined through LDS: a row that was cut into 170 parts is one workgroup's work (one lane group alone takes 110 us for it,
-// a load's latency for each part), many rows of a few parts are several to a workgroup.
+// Joins the splits' parts of each row.  D / 4 lanes take a part's row.  With GROUPS such groups a row is one workgroup's work
+// and each group takes every GROUPS-th part, joined through LDS (a row in 170 parts: 10 us; one group alone takes 110, a
+// load's latency for each part); many rows of a few parts each are several to a workgroup.
 template <int D, int GROUPS>
 __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(const CacheAttnArgs a) {
   constexpr int kLanes = D / 4, kRows = kThreads / kLanes / GROUPS;
@@ -765,7 +824,34 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(const CacheAt
 // ---------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------
-int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, CacheAttnPlan *plan) {
+// How many parts the keys of a row are cut into: the number with the least time by this model of the launch.
+//   A CU works through its workgroups one round after another: `slots` of them fit the chip, and the last round counts whole
+//   (a row tile's CU with one of them alone takes 1.6 times as long for it as for half of two).  Cutting evens that
+//   out; each part costs the writing and reading of its sums.
+// Measured, one call's keys in 1, 2, 3, 4 parts: 444 tiles of 128 rows, 32 760 keys, d 128: 1031, 1027, 1017, 928 us (the
+// model: 4); 1056 of 64 rows, 4 400 keys, d 64: 162, 142, 133, 133 us (3).  One token, 131 000 keys, 12 key heads: 21 parts
+// 77, 42 (504 workgroups, 512 fit) 77, 43: 104, 85: 81, 170: 88 us; 128 heads of up to 8 000 keys: 2: 42, 4: 35, 8: 37, 16: 44 us.
+static int splits_of(const CacheAttnPlan &plan, const Problem &pb, int max_blocks, bool lists) {
+  const bool few = plan.tile_rows == 32;
+  const double keys = (double)max_blocks * pb.block * (lists ? 0.25 : 1.0);     // lists: what they may keep
+  const int64_t slots = few ? (pb.d == 128 ? 512 : 1024) : 256;
+  // one unit's time: the cache's bytes at its share of 5.5 TB/s, or its products at a CU's share of 1000 / 600 TFLOP/s
+  const double unit = few ? 2.0 * keys * pb.d / (5.5e12 / slots) : 4.0 * plan.tile_rows * keys * pb.d / ((pb.d == 128 ? 1.0e15 : 0.6e15) / 256);
+  const double part = 8.0 * plan.units * plan.rows_kept * pb.d / 8e12;
+  int best = 1;
+  double best_time = 1e30;
+  for (int s = 1; s <= kMaxSplits && (s == 1 || (s * 256.0 <= keys && plan.units * s < kMostItems)); ++s) {
+    const double rounds = (double)((plan.units * s + slots - 1) / slots);
+    const double time = (few || rounds > 1.0 ? rounds : 1.6) / s * unit + (few ? rounds * 2e-6 : 0.0) + (s > 1 ? s * part + 3e-6 : 0.0);
+    if (time < best_time) {
+      best_time = time;
+      best = s;
+    }
+  }
+  return best;
+}
+
+int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, bool lists, CacheAttnPlan *plan) {
   const int group = pb.H / H_kv;
   const int64_t rows = (int64_t)(pb.L < pb.block ? pb.L : pb.block) * group;   // of one list
   plan->n_qblocks = pb.Nb;
@@ -773,14 +859,10 @@ int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, CacheAttnPlan *
   plan->tiles = (int)((rows + plan->tile_rows - 1) / plan->tile_rows);
   plan->rows_kept = (int)(rows < plan->tile_rows ? rows : plan->tile_rows);
   plan->units = (int64_t)pb.B * H_kv * pb.Nb * plan->tiles;
-  const int64_t wanted = plan->tile_rows == 32 ? 2048 : 512;
-  int64_t splits = wanted / plan->units;
-  const int64_t most = ((int64_t)max_blocks * pb.block + 255) / 256;
-  if (splits > most) splits = most;
-  if (splits > kMaxSplits) splits = kMaxSplits;
-  plan->splits = splits < 1 ? 1 : (int)splits;
-  if ((int64_t)pb.Nb * max_blocks >= ((int64_t)1 << 31)) return ASA_ERR_UNSUPPORTED;
-  return plan->units * plan->splits < ((int64_t)1 << 31) - 64 ? ASA_OK : ASA_ERR_UNSUPPORTED;
+  plan->splits = 1;
+  if ((int64_t)pb.Nb * max_blocks >= ((int64_t)1 << 31) || plan->units >= kMostItems) return ASA_ERR_UNSUPPORTED;
+  plan->splits = splits_of(*plan, pb, max_blocks, lists);
+  return ASA_OK;
 }
 
 size_t cache_attn_workspace_bytes(const Problem &pb, const CacheAttnPlan &plan) {
@@ -799,7 +881,7 @@ static hipError_t launch_cache_attn_as(const CacheAttnArgs &a, hipStream_t st) {
   if (e != hipSuccess || a.splits == 1) return e;
   constexpr int kGroups = kThreads / (D / 4);
   const int64_t rows = units * a.rows_kept;
-  if (a.splits > kFewSplits) cache_attn_join_kernel<D, kGroups><<<(int)rows, kThreads, 0, st>>>(a);
+  if (rows <= kFewRows) cache_attn_join_kernel<D, kGroups><<<(int)rows, kThreads, 0, st>>>(a);
   else cache_attn_join_kernel<D, 1><<<(int)((rows + kGroups - 1) / kGroups), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -66,7 +66,7 @@ struct CacheAttnPlan {
   int tiles, tile_rows, rows_kept, splits, n_qblocks;
   int64_t units;          // (sequence, key head, block of queries, row tile)
 };
-int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, CacheAttnPlan *plan);   // asa_status
+int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, bool lists, CacheAttnPlan *plan);   // asa_status
 size_t cache_attn_workspace_bytes(const Problem &pb, const CacheAttnPlan &plan);
 hipError_t launch_cache_attn(const CacheAttnArgs &a, int D, hipStream_t st);
 
