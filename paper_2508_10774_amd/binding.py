@@ -376,26 +376,40 @@ def _device(stream, first: torch.Tensor) -> int:
     return dev
 
 
+def _stream_on(stream, dev: int) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
 def _flat(t: Optional[torch.Tensor], what: str, dtype, n: int, dev: int) -> int:
     """Pointer of a contiguous tensor of (at least) n elements; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
-        raise AsaError(f"{what}: {n} contiguous elements of {dtype} on device {dev} expected, got {tuple(t.shape)} of "
-                       f"{t.dtype} on {t.device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.get_device() == dev and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
+    raise AsaError(f"{what}: {n} contiguous elements of {dtype} on device {dev} expected, got {tuple(t.shape)} of {t.dtype} "
+                   f"on {t.device}")
+
+
+def _packed(struct_type, layout, values):
+    try:
+        return struct_type.from_buffer_copy(layout.pack(*values))
+    except (struct.error, TypeError, OverflowError) as e:
+        raise AsaError(f"{struct_type.__name__}: {e}") from None
 
 
 def _rows(t: Optional[torch.Tensor], what: str, shape, stride, dev: int) -> int:
     """Pointer of a bf16 tensor [B, heads, L, d] that has the strides that the call gives for it; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not torch.bfloat16 or t.get_device() != dev or tuple(t.shape) != shape:
+    if t.dtype is not torch.bfloat16 or t.get_device() != dev or t.shape != shape:
         raise AsaError(f"{what}: bf16 {shape} on device {dev} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    B, H, L, d = shape
     s0, s1, s2 = stride
     if not (s0 or s1 or s2):
-        s0, s1, s2 = H * L * d, L * d, d
+        s2 = shape[3]
+        s1 = shape[2] * s2
+        s0 = shape[1] * s1
     got = t.stride()
     if got != (s0, s1, s2, 1) and any(n > 1 and a != b for n, a, b in zip(shape, got, (s0, s1, s2, 1))):
         raise AsaError(f"{what}: strides {(s0, s1, s2, 1)} expected, got {got}")
@@ -431,20 +445,21 @@ class QkNorm:
     def c(self, p: Params, dev: int) -> asa_qk_norm:
         if self.kind not in _KINDS or self.pairing not in _PAIRINGS:
             raise AsaError(f"kind {self.kind!r}: one of {list(_KINDS)}; pairing {self.pairing!r}: one of {list(_PAIRINGS)}")
-        f32, d, rows = torch.float32, p.d, 0
-        if self.rot_dim and self.cos is not None and self.sin is not None:
-            rows = min(self.cos.shape[0], self.sin.shape[0])
-            for x in (self.cos, self.sin):
-                if x.dim() != 2 or x.shape[1] * 2 != self.rot_dim:
-                    raise AsaError(f"cos, sin: [rows, {self.rot_dim // 2}] expected, got {tuple(x.shape)}")
-        n = rows * self.rot_dim // 2
-        return asa_qk_norm.from_buffer_copy(_PACKED_NORM.pack(
-            self.H_kv, _KINDS[self.kind], self.eps, self.rot_dim, _PAIRINGS[self.pairing], rows, self.first_row,
-            _flat(self.start, "start", torch.int32, p.B, dev),
-            _flat(self.cos, "cos", f32, n, dev), _flat(self.sin, "sin", f32, n, dev),
+        f32, d, rot = torch.float32, p.d, self.rot_dim
+        rows = cos = sin = 0
+        if rot and self.cos is not None and self.sin is not None:
+            shape = self.cos.shape
+            if len(shape) != 2 or shape[1] * 2 != rot or self.sin.shape != shape:
+                raise AsaError(f"cos, sin: [rows, {rot // 2}] expected, got {tuple(shape)} and {tuple(self.sin.shape)}")
+            rows = shape[0]
+            cos, sin = _flat(self.cos, "cos", f32, 0, dev), _flat(self.sin, "sin", f32, 0, dev)
+        q_out, k_out = self.q_out_stride, self.k_out_stride
+        return _packed(asa_qk_norm, _PACKED_NORM, (
+            self.H_kv, _KINDS[self.kind], self.eps, rot, _PAIRINGS[self.pairing], rows, self.first_row,
+            _flat(self.start, "start", torch.int32, p.B, dev), cos, sin,
             _flat(self.q_weight, "q_weight", f32, d, dev), _flat(self.k_weight, "k_weight", f32, d, dev),
             _flat(self.q_bias, "q_bias", f32, d, dev), _flat(self.k_bias, "k_bias", f32, d, dev),
-            *self.q_out_stride, *self.k_out_stride))
+            q_out[0], q_out[1], q_out[2], k_out[0], k_out[1], k_out[2]))
 
 
 def asa_qk_norm_rope(p: Params, n: QkNorm, q, k, q_out, k_out, stream=None):
@@ -453,7 +468,7 @@ def asa_qk_norm_rope(p: Params, n: QkNorm, q, k, q_out, k_out, stream=None):
     qs, ks = (p.B, p.H, p.L, p.d), (p.B, n.H_kv or p.H, p.L, p.d)
     _check(load().asa_qk_norm_rope(ctypes.byref(p.c()), ctypes.byref(n.c(p, dev)), _rows(q, "q", qs, p.q_stride, dev),
                                    _rows(k, "k", ks, p.k_stride, dev), _rows(q_out, "q_out", qs, n.q_out_stride, dev),
-                                   _rows(k_out, "k_out", ks, n.k_out_stride, dev), _stream(stream)), "asa_qk_norm_rope")
+                                   _rows(k_out, "k_out", ks, n.k_out_stride, dev), _stream_on(stream, dev)), "asa_qk_norm_rope")
 
 
 def asa_qk_norm_rope_bwd_workspace_bytes(p: Params, n: QkNorm) -> int:
@@ -474,7 +489,7 @@ def asa_qk_norm_rope_bwd(p: Params, n: QkNorm, q, k, dq_out, dk_out, dq, dk, dq_
         _flat(dq_weight, "dq_weight", f32, d, dev), _flat(dk_weight, "dk_weight", f32, d, dev),
         _flat(dq_bias, "dq_bias", f32, d, dev), _flat(dk_bias, "dk_bias", f32, d, dev),
         _flat(workspace, "workspace", torch.uint8, 0, dev), workspace.nbytes if workspace is not None else 0,
-        _stream(stream)), "asa_qk_norm_rope_bwd")
+        _stream_on(stream, dev)), "asa_qk_norm_rope_bwd")
 
 
 @dataclass
@@ -495,25 +510,26 @@ class KvCache:
         return self.k_scale.shape[2]
 
     def c(self, p: Params, dev: int) -> asa_kv_cache:
-        B, H, blocks = self.k_scale.shape
-        if B != p.B or self.v_scale.shape != self.k_scale.shape:
-            raise AsaError(f"cache of {tuple(self.k_scale.shape)} and {tuple(self.v_scale.shape)} blocks for {p.B} sequences")
-        n = B * H * blocks
-        codes = n * p.block * p.d
+        shape = self.k_scale.shape
+        B, H, blocks = shape
+        if B != p.B or self.v_scale.shape != shape:
+            raise AsaError(f"cache of {tuple(shape)} and {tuple(self.v_scale.shape)} blocks for {p.B} sequences")
+        codes = B * H * blocks * p.block * p.d
         if self.k.numel() != codes or self.v.numel() != codes:
             raise AsaError(f"cache: {codes} codes expected, got {self.k.numel()} and {self.v.numel()}")
-        return asa_kv_cache.from_buffer_copy(_PACKED_CACHE.pack(
-            H, blocks, _flat(self.k, "cache.k", torch.uint8, codes, dev), _flat(self.v, "cache.v", torch.uint8, codes, dev),
-            _flat(self.k_scale, "cache.k_scale", torch.float32, n, dev),
-            _flat(self.v_scale, "cache.v_scale", torch.float32, n, dev)))
+        u8, f32 = torch.uint8, torch.float32
+        return _packed(asa_kv_cache, _PACKED_CACHE, (
+            H, blocks, _flat(self.k, "cache.k", u8, 0, dev), _flat(self.v, "cache.v", u8, 0, dev),
+            _flat(self.k_scale, "cache.k_scale", f32, 0, dev), _flat(self.v_scale, "cache.v_scale", f32, 0, dev)))
 
 
 def _cache_call(fn, p: Params, c: KvCache, k, v, start, count, stream):
     dev = _device(stream, c.k)
-    shape = (p.B, c.H_kv, p.L, p.d)
+    B, i32 = p.B, torch.int32
+    shape = (B, c.H_kv, p.L, p.d)
     _check(getattr(load(), fn)(ctypes.byref(p.c()), ctypes.byref(c.c(p, dev)), _rows(k, "k", shape, p.k_stride, dev),
-                               _rows(v, "v", shape, p.v_stride, dev), _flat(start, "start", torch.int32, p.B, dev),
-                               _flat(count, "count", torch.int32, p.B, dev), _stream(stream)), fn)
+                               _rows(v, "v", shape, p.v_stride, dev), _flat(start, "start", i32, B, dev),
+                               _flat(count, "count", i32, B, dev), _stream_on(stream, dev)), fn)
 
 
 def asa_cache_write(p: Params, c: KvCache, k, v, start=None, count=None, stream=None):
@@ -535,13 +551,17 @@ def asa_attn_cache_workspace_bytes(p: Params, c: KvCache) -> int:
 def asa_attn_cache(p: Params, c: KvCache, length, q, row_ptr, col_idx, o, lse, workspace, stream=None):
     """q [B, H, L, d] attends to tokens [0, length[b]) of the cache, in the blocks of the lists if there are any."""
     dev = _device(stream, q)
-    shape, lists = (p.B, p.H, p.L, p.d), p.B * c.H_kv
+    shape, i32 = (p.B, p.H, p.L, p.d), torch.int32
+    ptr = idx = 0
+    if row_ptr is not None or col_idx is not None:
+        lists, rows = p.B * c.H_kv, p.Nb
+        ptr = _flat(row_ptr, "row_ptr", i32, lists * (rows + 1), dev)
+        idx = _flat(col_idx, "col_idx", i32, lists * rows * c.max_blocks, dev)
     _check(load().asa_attn_cache(
-        ctypes.byref(p.c()), ctypes.byref(c.c(p, dev)), _flat(length, "length", torch.int32, p.B, dev),
-        _rows(q, "q", shape, p.q_stride, dev), _flat(row_ptr, "row_ptr", torch.int32, lists * (p.Nb + 1), dev),
-        _flat(col_idx, "col_idx", torch.int32, lists * p.Nb * c.max_blocks, dev), _rows(o, "o", shape, p.o_stride, dev),
-        _flat(lse, "lse", torch.float32, p.B * p.H * p.L, dev), _flat(workspace, "workspace", torch.uint8, 0, dev),
-        workspace.nbytes if workspace is not None else 0, _stream(stream)), "asa_attn_cache")
+        ctypes.byref(p.c()), ctypes.byref(c.c(p, dev)), _flat(length, "length", i32, p.B, dev), _rows(q, "q", shape, p.q_stride, dev),
+        ptr, idx, _rows(o, "o", shape, p.o_stride, dev), _flat(lse, "lse", torch.float32, p.B * p.H * p.L, dev),
+        _flat(workspace, "workspace", torch.uint8, 0, dev), workspace.nbytes if workspace is not None else 0,
+        _stream_on(stream, dev)), "asa_attn_cache")
 
 
 def asa_mfma_rate_probe(workgroups: int, iters: int, sink, idle_sleep: int = 0, vector_stream: bool = False,

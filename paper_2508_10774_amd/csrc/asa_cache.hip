@@ -79,16 +79,18 @@ __device__ __forceinline__ f32x4 decode4(uint32_t codes) {
 #endif
 }
 
-// x / scale: exact by the reciprocal where the scale is a power of two, as those of the writer are
+// x / scale: exact by the reciprocal where the scale is a power of two, as those of the writer are (a division is ten
+// instructions).  EXACT is the caller's branch on is_power_of_two(scale).
+__device__ __forceinline__ bool is_power_of_two(float s) {
+  const uint32_t bits = __builtin_bit_cast(uint32_t, s), e = bits >> 23;
+  return (bits & 0x7fffffu) == 0 && e >= 1 && e <= 253;
+}
+template <bool EXACT>
 struct Divider {
   float scale, reciprocal;
-  bool exact;
-  __device__ __forceinline__ explicit Divider(float s) : scale(s) {
-    const uint32_t bits = __builtin_bit_cast(uint32_t, s), e = bits >> 23;
-    exact = (bits & 0x7fffffu) == 0 && e >= 1 && e <= 253;
-    reciprocal = exact ? __builtin_bit_cast(float, (254u - e) << 23) : 0.f;
-  }
-  __device__ __forceinline__ float operator()(float x) const { return exact ? x * reciprocal : x / scale; }
+  __device__ __forceinline__ explicit Divider(float s)
+      : scale(s), reciprocal(__builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, s))) {}
+  __device__ __forceinline__ float operator()(float x) const { return EXACT ? x * reciprocal : x / scale; }
 };
 
 // bytes of a dword whose tokens t0 .. t0 + 3 lie in [lo, hi)
@@ -108,6 +110,49 @@ __device__ __forceinline__ int v_place(int quad, int channel) {
   return quad / 8 * (32 * D) + channel / 32 * 1024 + quad % 2 * 512 + channel % 32 * 16 + quad % 8 / 2 * 4;
 }
 
+// Where a block's 16-byte piece p lies in LDS while the block is put together: the pieces that the lanes of one store go to are
+// a multiple of 8 apart, which without this is the same few banks.
+__device__ __forceinline__ int image_piece(int p) { return p ^ ((p >> 3 & 7) | (p >> 6 & 1) << 3); }
+__device__ __forceinline__ int image_at(int byte) { return image_piece(byte >> 4) << 4 | (byte & 15); }
+
+// The four tokens `raw` (8 channels each) of a thread as codes in the block's image.
+template <int D, bool EXACT>
+__device__ __forceinline__ void encode_unit(const u32x4 (&raw)[4], bool odd, float scale, bool transposed, int quad, int chunk,
+                                            unsigned char *image) {
+  const Divider<EXACT> by(scale);
+  float x[4][8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      float lo = __builtin_bit_cast(float, raw[j][w] << 16), hi = __builtin_bit_cast(float, raw[j][w] & 0xffff0000u);
+      if (odd) {
+        if (__builtin_isinf(lo)) lo = __builtin_nanf("");
+        if (__builtin_isinf(hi)) hi = __builtin_nanf("");
+      }
+      x[j][2 * w] = by(lo);
+      x[j][2 * w + 1] = by(hi);
+    }
+  if (transposed) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      *reinterpret_cast<uint32_t *>(image + image_at(v_place<D>(quad, chunk * 8 + c))) = encode4(x[0][c], x[1][c], x[2][c], x[3][c]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uint2 *>(image + image_at(k_place<D>(quad * 4 + j, chunk))) =
+          uint2{encode4(x[j][0], x[j][1], x[j][2], x[j][3]), encode4(x[j][4], x[j][5], x[j][6], x[j][7])};
+  }
+}
+// The held codes among four, written again for another scale.
+template <bool EXACT>
+__device__ __forceinline__ uint32_t recoded(uint32_t codes, uint32_t which, float old_scale, float scale) {
+  const Divider<EXACT> by(scale);
+  const f32x4 was = decode4(codes);
+  const uint32_t now = encode4(by(was[0] * old_scale), by(was[1] * old_scale), by(was[2] * old_scale), by(was[3] * old_scale));
+  return (now & which) | (codes & ~which);
+}
+
 }  // namespace
 
 // One workgroup for each block that new tokens go to: the rows come in 16 bytes to a lane (four tokens of 8
@@ -115,8 +160,12 @@ __device__ __forceinline__ int v_place(int quad, int channel) {
 // 16 bytes to a lane.  Bytes of a block that are not new are read only where they share 16 bytes with
 // new ones, or where the scale grew and the tokens held are coded again.
 template <int D, int BLOCK>
-__global__ __launch_bounds__(kThreads) void cache_write_kernel(const CacheArgs a) {
-  constexpr int kChunks = D / 8, kUnits = BLOCK / 4 * kChunks, kPer = (kUnits + kThreads - 1) / kThreads;
+constexpr int cache_threads() { return BLOCK * D / 32 < kThreads ? BLOCK * D / 32 : kThreads; }   // 32 values a thread at least
+
+template <int D, int BLOCK>
+__global__ __launch_bounds__((cache_threads<D, BLOCK>())) void cache_write_kernel(const CacheArgs a) {
+  constexpr int kThreads = cache_threads<D, BLOCK>(), kChunks = D / 8, kPer = BLOCK / 4 * kChunks / kThreads;
+  constexpr int kPieces = BLOCK * D / 16 / kThreads;      // of 16 bytes, in a thread
   const BlockItem it = block_item(a, BLOCK, true);
   if (!it.any) return;
   const CacheSide &side = a.side[it.side];
@@ -136,9 +185,16 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(const CacheArgs a
     for (int j = 0; j < 4; ++j) {
       const int t = quad * 4 + j;
       raw[i][j] = u32x4{0, 0, 0, 0};
-      if (u < kUnits && t >= it.lo && t < it.hi)
+      if (t >= it.lo && t < it.hi)
         raw[i][j] = *reinterpret_cast<const u32x4 *>(rows + (it.row0 + t) * side.view.sL + chunk * 8);
     }
+  }
+  // bytes that are kept, on their way while the scale is formed: of a block that is written whole there are none
+  const bool whole = it.lo == 0 && it.hi == BLOCK;
+  u32x4 old[kPieces];
+  if (!whole) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) old[i] = *reinterpret_cast<const u32x4 *>(codes + (threadIdx.x + i * kThreads) * 16);
   }
 #pragma unroll
   for (int i = 0; i < kPer; ++i)
@@ -176,81 +232,51 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(const CacheArgs a
   const float needed = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
   const float scale = held && old_scale > needed ? old_scale : needed;
   const bool recode = held && scale != old_scale;
-  const Divider by(scale);
+  const bool exact = __builtin_amdgcn_readfirstlane(is_power_of_two(scale));
 
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int u = threadIdx.x + i * kThreads, quad = u / kChunks, chunk = u % kChunks;
-    if (u >= kUnits) break;
-    float x[4][8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        float lo = __builtin_bit_cast(float, raw[i][j][w] << 16), hi = __builtin_bit_cast(float, raw[i][j][w] & 0xffff0000u);
-        if (odd) {
-          if (__builtin_isinf(lo)) lo = __builtin_nanf("");
-          if (__builtin_isinf(hi)) hi = __builtin_nanf("");
-        }
-        x[j][2 * w] = by(lo);
-        x[j][2 * w + 1] = by(hi);
-      }
-    if (side.transposed) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        *reinterpret_cast<uint32_t *>(image + v_place<D>(quad, chunk * 8 + c)) = encode4(x[0][c], x[1][c], x[2][c], x[3][c]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t *to = reinterpret_cast<uint32_t *>(image + k_place<D>(quad * 4 + j, chunk));
-        to[0] = encode4(x[j][0], x[j][1], x[j][2], x[j][3]);
-        to[1] = encode4(x[j][4], x[j][5], x[j][6], x[j][7]);
-      }
-    }
+    if (quad * 4 + 3 < it.lo || quad * 4 >= it.hi) continue;
+    if (exact) encode_unit<D, true>(raw[i], odd, scale, side.transposed, quad, chunk, image);
+    else encode_unit<D, false>(raw[i], odd, scale, side.transposed, quad, chunk, image);
   }
   __syncthreads();
   if (threadIdx.x == 0) *scale_at = scale;
 
-  constexpr int kPieces = BLOCK * D / 16;
+  if (whole) {
 #pragma unroll
-  for (int i = 0; i < (kPieces + kThreads - 1) / kThreads; ++i) {
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = (threadIdx.x + i * kThreads) * 16;
+      *reinterpret_cast<u32x4 *>(codes + at) = *reinterpret_cast<const u32x4 *>(image + image_at(at));
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
     const int piece = threadIdx.x + i * kThreads;
-    if (piece >= kPieces) break;
     const int t_first = piece / (2 * D) * 32 + (side.transposed ? piece / 32 % 2 * 4 : piece % 32);
-    uint32_t fresh[4], again[4], all = ~0u, any = 0;
+    u32x4 value = *reinterpret_cast<const u32x4 *>(image + image_at(piece * 16));
+    uint32_t any = 0;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       // (a piece of K is 16 channels of one token)
-      fresh[m] = side.transposed ? bytes_within(t_first + 8 * m, it.lo, it.hi)
-                                 : (t_first >= it.lo && t_first < it.hi ? ~0u : 0u);
-      again[m] = !recode ? 0u : side.transposed ? bytes_within(t_first + 8 * m, 0, it.lo) : (t_first < it.lo ? ~0u : 0u);
-      all &= fresh[m];
-      any |= fresh[m] | again[m];
+      const uint32_t fresh = side.transposed ? bytes_within(t_first + 8 * m, it.lo, it.hi)
+                                             : (t_first >= it.lo && t_first < it.hi ? ~0u : 0u);
+      const uint32_t again = !recode ? 0u : side.transposed ? bytes_within(t_first + 8 * m, 0, it.lo) : (t_first < it.lo ? ~0u : 0u);
+      any |= fresh | again;
+      uint32_t kept = old[i][m];
+      if (again) kept = exact ? recoded<true>(kept, again, old_scale, scale) : recoded<false>(kept, again, old_scale, scale);
+      value[m] = (value[m] & fresh) | (kept & ~fresh);
     }
-    if (!any) continue;
-    u32x4 *at = reinterpret_cast<u32x4 *>(codes + piece * 16);
-    u32x4 value = *reinterpret_cast<const u32x4 *>(image + piece * 16);
-    if (all != ~0u) {
-      const u32x4 old = *at;
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        uint32_t kept = old[m];
-        if (again[m]) {
-          const f32x4 was = decode4(old[m]);
-          const uint32_t now = encode4(by(was[0] * old_scale), by(was[1] * old_scale), by(was[2] * old_scale), by(was[3] * old_scale));
-          kept = (now & again[m]) | (kept & ~again[m]);
-        }
-        value[m] = (value[m] & fresh[m]) | (kept & ~fresh[m]);
-      }
-    }
-    *at = value;
+    if (any) *reinterpret_cast<u32x4 *>(codes + piece * 16) = value;
   }
 }
 
 // One workgroup for each block that the call reads from; a thread writes 16 bytes of a row (K) or of four rows (V).
 template <int D, int BLOCK>
-__global__ __launch_bounds__(kThreads) void cache_read_kernel(const CacheArgs a) {
-  constexpr int kChunks = D / 8;
+__global__ __launch_bounds__((cache_threads<D, BLOCK>())) void cache_read_kernel(const CacheArgs a) {
+  constexpr int kThreads = cache_threads<D, BLOCK>(), kChunks = D / 8;
   const BlockItem it = block_item(a, BLOCK, false);
   if (!it.any) return;
   const CacheSide &side = a.side[it.side];
@@ -258,37 +284,46 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(const CacheArgs a)
   const float scale = side.scale[slab * a.max_blocks + it.j];
   const unsigned char *codes = reinterpret_cast<const unsigned char *>(side.codes) + (slab * a.max_blocks + it.j) * (BLOCK * D);
   bf16 *rows = reinterpret_cast<bf16 *>(side.rows) + it.b * side.view.sB + it.h * side.view.sH;
+  // (all loads of a thread in front of the first use: the block is the cache's own, whichever of its tokens are asked for)
   if (side.transposed) {
-    constexpr int kUnits = BLOCK / 4 * kChunks, kPer = (kUnits + kThreads - 1) / kThreads;
+    constexpr int kPer = BLOCK / 4 * kChunks / kThreads;
+    uint32_t raw[kPer][8];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int u = threadIdx.x + i * kThreads, quad = u / kChunks, chunk = u % kChunks;
-      if (u >= kUnits || quad * 4 + 3 < it.lo || quad * 4 >= it.hi) continue;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) raw[i][c] = *reinterpret_cast<const uint32_t *>(codes + v_place<D>(quad, chunk * 8 + c));
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int u = threadIdx.x + i * kThreads, quad = u / kChunks, chunk = u % kChunks;
       f32x4 x[8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) x[c] = decode4(*reinterpret_cast<const uint32_t *>(codes + v_place<D>(quad, chunk * 8 + c)));
+      for (int c = 0; c < 8; ++c) x[c] = decode4(raw[i][c]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int t = quad * 4 + j;
-        if (t < it.lo || t >= it.hi) continue;
         u32x4 out;
 #pragma unroll
         for (int w = 0; w < 4; ++w) out[w] = pack_bf16x2(x[2 * w][j] * scale, x[2 * w + 1][j] * scale);
-        *reinterpret_cast<u32x4 *>(rows + (it.row0 + t) * side.view.sL + chunk * 8) = out;
+        if (t >= it.lo && t < it.hi) *reinterpret_cast<u32x4 *>(rows + (it.row0 + t) * side.view.sL + chunk * 8) = out;
       }
     }
   } else {
-    constexpr int kUnits = BLOCK * kChunks;
-    static_assert(kUnits % kThreads == 0, "whole rounds");
+    constexpr int kPer = BLOCK * kChunks / kThreads;
+    uint2 raw[kPer];
 #pragma unroll
-    for (int i = 0; i < kUnits / kThreads; ++i) {
+    for (int i = 0; i < kPer; ++i) {
+      const int u = threadIdx.x + i * kThreads;
+      raw[i] = *reinterpret_cast<const uint2 *>(codes + k_place<D>(u / kChunks, u % kChunks));
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
       const int u = threadIdx.x + i * kThreads, t = u / kChunks, chunk = u % kChunks;
-      if (t < it.lo || t >= it.hi) continue;
-      const uint32_t *at = reinterpret_cast<const uint32_t *>(codes + k_place<D>(t, chunk));
-      const f32x4 lo = decode4(at[0]), hi = decode4(at[1]);
-      *reinterpret_cast<u32x4 *>(rows + (it.row0 + t) * side.view.sL + chunk * 8) =
-          u32x4{pack_bf16x2(lo[0] * scale, lo[1] * scale), pack_bf16x2(lo[2] * scale, lo[3] * scale),
-                pack_bf16x2(hi[0] * scale, hi[1] * scale), pack_bf16x2(hi[2] * scale, hi[3] * scale)};
+      const f32x4 lo = decode4(raw[i].x), hi = decode4(raw[i].y);
+      const u32x4 out = {pack_bf16x2(lo[0] * scale, lo[1] * scale), pack_bf16x2(lo[2] * scale, lo[3] * scale),
+                         pack_bf16x2(hi[0] * scale, hi[1] * scale), pack_bf16x2(hi[2] * scale, hi[3] * scale)};
+      if (t >= it.lo && t < it.hi) *reinterpret_cast<u32x4 *>(rows + (it.row0 + t) * side.view.sL + chunk * 8) = out;
     }
   }
 }
@@ -893,8 +928,9 @@ hipError_t launch_cache_attn(const CacheAttnArgs &a, int D, hipStream_t st) {
 template <int D, int BLOCK>
 static hipError_t launch_cache_as(const CacheArgs &a, bool write, hipStream_t st) {
   const int grid = a.reached * a.H * a.B * a.n_sides;
-  if (write) cache_write_kernel<D, BLOCK><<<grid, kThreads, 0, st>>>(a);
-  else cache_read_kernel<D, BLOCK><<<grid, kThreads, 0, st>>>(a);
+  constexpr int threads = cache_threads<D, BLOCK>();
+  if (write) cache_write_kernel<D, BLOCK><<<grid, threads, 0, st>>>(a);
+  else cache_read_kernel<D, BLOCK><<<grid, threads, 0, st>>>(a);
   return hipGetLastError();
 }
 static hipError_t launch_cache(const CacheArgs &a, int D, int block, bool write, hipStream_t st) {
