@@ -337,6 +337,9 @@ constexpr int kMaxSplits = kThreads;
 constexpr int64_t kMostItems = ((int64_t)1 << 31) - 64;   // workgroups of a launch
 constexpr int64_t kFewRows = 4096;   // up to here the join has a workgroup for each row
 constexpr float kLn2 = 0.6931471805599453f;
+// What a row's maximum may grow by before its sums are brought down to it (log2 units): probabilities are then up to 2^8 instead
+// of 1, which costs no precision, and the sums' D multiplications are rare instead of in nearly every step.
+constexpr float kSlack = 8.f;
 constexpr float kLeastFactor = 1.17549435e-38f;   // (a factor of zero would make NaN of a masked score)
 
 // The two A operands that 16 codes of a tile are.
@@ -444,8 +447,7 @@ struct Rows {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
     const float m_new = fmaxf(m, max_of_halves(top) * bs.c);
-    const float down = bs.log2_v - m_new;
-    if (__ballot(m_new != m)) {
+    if (__ballot(m_new - m > kSlack)) {
       const float shrink = fast_exp2(m - m_new);
       l *= shrink;
 #pragma unroll
@@ -454,6 +456,7 @@ struct Rows {
         for (int i = 0; i < 16; ++i) acc[t][i] *= shrink;
       m = m_new;
     }
+    const float down = bs.log2_v - m;
     float sum = 0.f;
 #pragma unroll
     for (int n = 0; n < NG; ++n) {
@@ -527,33 +530,40 @@ struct Walk {
     at = (int)min((int64_t)split * share, (int64_t)n);
     end = min(at + share, n);
   }
-  // block at a position; negative where the list names none that the sequence has
-  __device__ __forceinline__ int block(int position) const {
-    const int j = list ? uniform_read(list + position) : position;
-    return j >= 0 && j < n_blocks ? j : -1;
-  }
+  // what stands at a position; the block there, negative where the list names none that the sequence has
+  __device__ __forceinline__ int entry(int position) const { return list ? uniform_read(list + position) : position; }
+  __device__ __forceinline__ int block(int e) const { return e >= 0 && e < n_blocks ? e : -1; }
 };
 
 // Steps of KEYS keys along a walk, STRIDE apart: those that are full, one after the other; the one that the sequence ends
 // in (there is one at most) is kept for the end, so that the loop over the others need not mask.
 template <int BLOCK, int KEYS, int STRIDE>
 struct Steps {
-  static constexpr int kPerBlock = BLOCK / KEYS;
+  static constexpr int kPerBlock = BLOCK / KEYS, kAhead = STRIDE > kPerBlock ? STRIDE / kPerBlock : 1;   // (in positions)
   const Walk &walk;
   const CacheAttnArgs &a;
   int64_t block0;
   int x, end, j;              // step, its block
   float k_scale, v_scale;     // of the block, on their way while the step before is worked on
   int last_x, last_j;
+  int position, ahead;        // of the walk; the list's entry kAhead further on, on its way
   __device__ __forceinline__ Steps(const CacheAttnArgs &a_, const Walk &w, int64_t block0_, int first)
-      : walk(w), a(a_), block0(block0_), end(w.end * kPerBlock), j(0), k_scale(1.f), v_scale(1.f), last_x(-1), last_j(0) {
-    find(w.at * kPerBlock + first);
+      : walk(w), a(a_), block0(block0_), end(w.end * kPerBlock), j(-1), k_scale(1.f), v_scale(1.f), last_x(-1), last_j(0),
+        position(-1), ahead(0) {
+    x = w.at * kPerBlock + first;
+    if (x >= end) return;
+    ahead = w.entry(x / kPerBlock);
+    find(x);
   }
   __device__ __forceinline__ bool any() const { return x < end; }
   __device__ __forceinline__ void advance() { find(x + STRIDE); }
   __device__ __forceinline__ void find(int from) {
     for (x = from; x < end; x += STRIDE) {
-      j = __builtin_amdgcn_readfirstlane(walk.block(x / kPerBlock));
+      if (x / kPerBlock != position) {
+        position = x / kPerBlock;
+        j = __builtin_amdgcn_readfirstlane(walk.block(ahead));
+        ahead = walk.entry(min(position + kAhead, walk.end - 1));
+      }
       if (j < 0) continue;
       const int left = walk.length - keys_before();
       if (left >= KEYS) {
