@@ -314,7 +314,9 @@ typedef struct asa_qk_norm {
  * q [B, H, L, d], k [B, H_kv, L, d] bf16 with p's q_stride and k_stride (slices of one projection
  * [B, L, heads * d], say) -> q_out, k_out bf16.  k = k_out = NULL: queries alone.  Of `p` only
  * B, H, L, d, q_stride and k_stride have a meaning.  L <= 131 072.  A tensor may be its own output
- * where the strides agree; any other overlap is undefined.
+ * where the strides agree; any other overlap is undefined.  Here and in the calls below the rows of a
+ * tensor that is written must lie apart (a stride of 0, for one: ASA_ERR_INVALID_ARG); tensors that are
+ * only read may repeat rows.
  */
 int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k,
                      void *q_out, void *k_out, void *hip_stream);
@@ -346,7 +348,8 @@ int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *
  *   v  [B, H_kv, max_blocks, block/32, d/32, 2, 32, 16]  token 8 m + 4 h + j, channel 32 c + x at
  *                                                        [c][h][x][4 m + j]  (m, j < 4; h < 2)
  *   k_scale, v_scale  [B, H_kv, max_blocks] fp32, positive
- * Token l of a sequence is token l % block of block l / block.
+ * Token l of a sequence is token l % block of block l / block.  A sequence that begins behind positions
+ * that were never written needs codes and scales there that mean something: code 0 and 2^-100, say.
  */
 typedef struct asa_kv_cache {
   int32_t H_kv;              /* key heads                                                        */

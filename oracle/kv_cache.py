@@ -104,7 +104,7 @@ class Cache:
     def __init__(self, B, H, blocks, block, d):
         self.block, self.blocks = block, blocks
         self.codes = {n: np.zeros((B, H, blocks, block, d), np.uint8) for n in "kv"}
-        self.scale = {n: np.ones((B, H, blocks)) for n in "kv"}
+        self.scale = {n: np.full((B, H, blocks), 2.0 ** LEAST_EXP) for n in "kv"}
 
     def write(self, name, x, start, count):
         B, H, L, _ = x.shape

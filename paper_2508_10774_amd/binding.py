@@ -604,9 +604,10 @@ def alloc_workspace(nbytes: int, device="cuda") -> torch.Tensor:
 
 
 def alloc_kv_cache(B: int, H_kv: int, max_blocks: int, d: int, block: int, device="cuda") -> KvCache:
-    """An empty cache: room for max_blocks * block tokens of each sequence."""
+    """An empty cache: room for max_blocks * block tokens of each sequence, all zeros at the scale that the writer gives zeros (a
+    larger one would stay where a sequence begins behind tokens that were never written, and cost what follows its precision)."""
     lead = (B, H_kv, max_blocks)
-    return KvCache(k=torch.zeros(*lead, block // 32, d // 16, 32, 16, dtype=torch.uint8, device=device),
-                   v=torch.zeros(*lead, block // 32, d // 32, 2, 32, 16, dtype=torch.uint8, device=device),
-                   k_scale=torch.ones(lead, dtype=torch.float32, device=device),
-                   v_scale=torch.ones(lead, dtype=torch.float32, device=device))
+    k = torch.zeros(*lead, block // 32, d // 16, 32, 16, dtype=torch.uint8, device=device)
+    v = torch.zeros(*lead, block // 32, d // 32, 2, 32, 16, dtype=torch.uint8, device=device)
+    k_scale, v_scale = (torch.full(lead, 2.0 ** -100, dtype=torch.float32, device=device) for _ in range(2))
+    return KvCache(k, v, k_scale, v_scale)

@@ -578,7 +578,23 @@ static int resolve_shape(const asa_params *p, int H, int block, Problem *pb) {
   return resolve(&shape, pb);
 }
 
-static int check_norm(const asa_params *p, const asa_qk_norm *n, NormArgs *a) {
+// The rows of a tensor that is written are apart from each other: along the axes in the order of their strides, each stride
+// passes all that lies inside (a stride of 0 would have several workgroups write one row).
+static bool rows_apart(const TensorView &v, const Problem &pb) {
+  struct { int64_t stride, n; } axis[3] = {{v.sB, pb.B}, {v.sH, pb.H}, {v.sL, pb.L}};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (axis[j].stride > axis[j + 1].stride) std::swap(axis[j], axis[j + 1]);
+  int64_t inside = pb.d;
+  for (const auto &x : axis) {
+    if (x.n == 1) continue;
+    if (x.stride < inside) return false;
+    inside += (x.n - 1) * x.stride;
+  }
+  return true;
+}
+
+static int check_norm(const asa_params *p, const asa_qk_norm *n, bool backward, NormArgs *a) {
   if (!p || !n) return ASA_ERR_INVALID_ARG;
   Problem q, k;
   int rc = resolve_shape(p, p->H, 128, &q);
@@ -601,6 +617,8 @@ static int check_norm(const asa_params *p, const asa_qk_norm *n, NormArgs *a) {
   if (!view_from(p->q_stride, q, &a->side[0].in) || !view_from(n->q_out_stride, q, &a->side[0].out) ||
       !view_from(p->k_stride, k, &a->side[1].in) || !view_from(n->k_out_stride, k, &a->side[1].out))
     return ASA_ERR_INVALID_ARG;
+  if (!rows_apart(backward ? a->side[0].in : a->side[0].out, q) || !rows_apart(backward ? a->side[1].in : a->side[1].out, k))
+    return ASA_ERR_INVALID_ARG;
   a->side[0].heads = q.H; a->side[0].w = n->q_weight; a->side[0].b = n->q_bias;
   a->side[1].heads = k.H; a->side[1].w = n->k_weight; a->side[1].b = n->k_bias;
   a->start = n->start; a->cos_table = n->cos_table; a->sin_table = n->sin_table;
@@ -612,7 +630,7 @@ static int check_norm(const asa_params *p, const asa_qk_norm *n, NormArgs *a) {
 int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k, void *q_out, void *k_out,
                      void *hip_stream) {
   NormArgs a;
-  int rc = check_norm(p, n, &a);
+  int rc = check_norm(p, n, false, &a);
   if (rc != ASA_OK) return rc;
   if (!q || !q_out || (k == nullptr) != (k_out == nullptr)) return ASA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return ASA_ERR_INVALID_ARG;
@@ -626,7 +644,7 @@ int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, c
 
 size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n) {
   NormArgs a;
-  if (check_norm(p, n, &a) != ASA_OK || plan_norm(&a, p->d) != ASA_OK) return 0;
+  if (check_norm(p, n, true, &a) != ASA_OK || plan_norm(&a, p->d) != ASA_OK) return 0;
   return round256(norm_partial_bytes(a.side[0], p->d)) + round256(norm_partial_bytes(a.side[1], p->d));
 }
 
@@ -634,7 +652,7 @@ int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *
                          const void *dk_out, void *dq, void *dk, float *dq_weight, float *dk_weight, float *dq_bias,
                          float *dk_bias, void *workspace, size_t workspace_bytes, void *hip_stream) {
   NormArgs a;
-  int rc = check_norm(p, n, &a);
+  int rc = check_norm(p, n, true, &a);
   if (rc != ASA_OK) return rc;
   if (!q || !dq_out || !dq || (k == nullptr) != (dk_out == nullptr) || (k == nullptr) != (dk == nullptr))
     return ASA_ERR_INVALID_ARG;
@@ -667,7 +685,7 @@ static int check_cache(const asa_params *p, const asa_kv_cache *c, bool need_k, 
 }
 
 static int cache_args(const asa_params *p, const asa_kv_cache *c, const void *k, const void *v, const int32_t *start,
-                      const int32_t *count, CacheArgs *a) {
+                      const int32_t *count, bool rows_written, CacheArgs *a) {
   int rc = check_cache(p, c, k != nullptr, v != nullptr);
   if (rc != ASA_OK) return rc;
   Problem pb;
@@ -677,6 +695,7 @@ static int cache_args(const asa_params *p, const asa_kv_cache *c, const void *k,
   memset(a, 0, sizeof(*a));
   TensorView kv, vv;
   if (!view_from(p->k_stride, pb, &kv) || !view_from(p->v_stride, pb, &vv)) return ASA_ERR_INVALID_ARG;
+  if (rows_written && ((k && !rows_apart(kv, pb)) || (v && !rows_apart(vv, pb)))) return ASA_ERR_INVALID_ARG;
   if (k) a->side[a->n_sides++] = CacheSide{c->k, c->k_scale, const_cast<void *>(k), kv, false};
   if (v) a->side[a->n_sides++] = CacheSide{c->v, c->v_scale, const_cast<void *>(v), vv, true};
   a->start = start; a->count = count;
@@ -691,7 +710,7 @@ static int cache_args(const asa_params *p, const asa_kv_cache *c, const void *k,
 int asa_cache_write(const asa_params *p, const asa_kv_cache *c, const void *k, const void *v, const int32_t *start,
                     const int32_t *count, void *hip_stream) {
   CacheArgs a;
-  int rc = cache_args(p, c, k, v, start, count, &a);
+  int rc = cache_args(p, c, k, v, start, count, false, &a);
   if (rc != ASA_OK) return rc;
   return finish(launch_cache_write(a, p->d, p->block, reinterpret_cast<hipStream_t>(hip_stream)));
 }
@@ -699,7 +718,7 @@ int asa_cache_write(const asa_params *p, const asa_kv_cache *c, const void *k, c
 int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v, const int32_t *start, const int32_t *count,
                    void *hip_stream) {
   CacheArgs a;
-  int rc = cache_args(p, c, k, v, start, count, &a);
+  int rc = cache_args(p, c, k, v, start, count, true, &a);
   if (rc != ASA_OK) return rc;
   return finish(launch_cache_read(a, p->d, p->block, reinterpret_cast<hipStream_t>(hip_stream)));
 }
@@ -710,7 +729,8 @@ static int check_cache_attn(const asa_params *p, const asa_kv_cache *c, bool lis
   if (rc != ASA_OK) return rc;
   if (p->scale != p->scale || p->scale < 0.f || isinf(p->scale)) return ASA_ERR_INVALID_ARG;
   pb->scale = p->scale == 0.f ? 1.0f / sqrtf((float)p->d) : p->scale;
-  if (!view_from(p->q_stride, *pb, &pb->q) || !view_from(p->o_stride, *pb, &pb->o)) return ASA_ERR_INVALID_ARG;
+  if (!view_from(p->q_stride, *pb, &pb->q) || !view_from(p->o_stride, *pb, &pb->o) || !rows_apart(pb->o, *pb))
+    return ASA_ERR_INVALID_ARG;
   if (c->H_kv < 1 || c->max_blocks < 1 || pb->H % c->H_kv) return ASA_ERR_INVALID_ARG;
   if (c->max_blocks > 65536) return ASA_ERR_UNSUPPORTED;
   return plan_cache_attn(*pb, c->H_kv, c->max_blocks, lists, plan);

@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kHeads = 4;      // heads of a token that a group of lanes takes at once
 constexpr int kThreads = 256;
-constexpr int kMaxGroups = 1024;   // workgroups of the backward for each of Q and K: what its partial sums cost
+constexpr int kMaxGroups = 512;    // workgroups of the backward for each of Q and K, each with a row of partial sums
 
 enum Pairing { kAdjacent = ASA_ROPE_ADJACENT, kHalves = ASA_ROPE_HALVES, kNone = 2 };
 

@@ -59,6 +59,10 @@ def test_norm_refusals():
     for args in (dict(q=None), dict(k=None), dict(gq=None), dict(gk=None), dict(dq=None), dict(dk=None), dict(qb=FAKE), dict(kb=FAKE),
                  dict(k=None, gk=None, dk=None), dict(qw=ctypes.c_void_p(0x10002)), dict(gq=odd), dict(dk=odd)):
         assert bwd(**args) == INVALID, args
+    # rows that are written lie apart: a stride of 0, heads inside one another, tokens inside a head
+    for bad in ((0, 6400, 64), (25600, 0, 64), (25600, 64, 64), (25600, 6392, 64)):
+        assert fwd(_params(), _norm(q_out_stride=bad)) == INVALID, bad
+        assert L.asa_qk_norm_rope_bwd(_params(q_stride=bad), _norm(), *[FAKE] * 8, None, None, None, 0, None) == INVALID, bad
     need = ws(_params(), _norm())
     assert bwd(w=None) == bwd(size=need - 1) == bwd(w=odd) == WORKSPACE
 
@@ -75,6 +79,8 @@ def test_cache_refusals():
             assert call(p=_params(**bad)) == INVALID, bad
         for bad in (dict(d=32), dict(block=32), dict(L=65537)):
             assert call(p=_params(**bad)) == UNSUPPORTED, bad
+        if fn is L.asa_cache_read:
+            assert call(p=_params(k_stride=(0, 6400, 64))) == call(p=_params(v_stride=(12800, 64, 64))) == INVALID
         odd = ctypes.c_void_p(0x10008)
         assert call(k=odd) == call(v=odd) == call(s=ctypes.c_void_p(0x10001)) == call(n=ctypes.c_void_p(0x10002)) == INVALID
 
@@ -86,6 +92,7 @@ def test_cached_attention_refusals():
         return L.asa_attn_cache(p, c, length, q, ptr, idx, o, lse, w, size, None)
 
     ws = L.asa_attn_cache_workspace_bytes
+    assert call(p=_params(o_stride=(0, 6400, 64))) == call(p=_params(o_stride=(25600, 32, 64))) == INVALID
     assert ws(_params(L=1), _cache(max_blocks=1000)) > 0
     for args in (dict(p=None), dict(c=None), dict(length=None), dict(q=None), dict(o=None), dict(lse=None), dict(ptr=FAKE), dict(idx=FAKE),
                  dict(q=ctypes.c_void_p(0x10008)), dict(o=ctypes.c_void_p(0x10004)), dict(lse=ctypes.c_void_p(0x10002)),
