@@ -769,7 +769,7 @@ int asa_attn_cache(const asa_params *p, const asa_kv_cache *c, const int32_t *le
   a.qv = pb.q; a.ov = pb.o;
   a.B = pb.B; a.H = pb.H; a.H_kv = c->H_kv; a.group = pb.H / c->H_kv; a.L = pb.L; a.block = pb.block;
   a.max_blocks = c->max_blocks; a.n_qblocks = plan.n_qblocks; a.tiles = plan.tiles; a.tile_rows = plan.tile_rows;
-  a.rows_kept = plan.rows_kept; a.splits = plan.splits;
+  a.rows_kept = plan.rows_kept; a.splits = plan.splits; a.units = (int)plan.units;
   a.scale_log2 = pb.scale * 1.4426950408889634f;
   return finish(launch_cache_attn(a, pb.d, reinterpret_cast<hipStream_t>(hip_stream)));
 }

@@ -59,7 +59,7 @@ struct CacheAttnArgs {
   int n_qblocks;          // blocks of queries
   int tiles, tile_rows;   // row tiles of a block of queries, rows of a tile
   int rows_kept;          // rows of a tile that exist, at most (pitch of `partial`)
-  int splits;
+  int splits, units;      // units: (sequence, key head, block of queries, row tile)
   float scale_log2;       // scale * log2(e)
 };
 struct CacheAttnPlan {
