@@ -867,25 +867,35 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(const CacheAt
 // ---------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------
-// How many parts the keys of a row are cut into: the number with the least time by this model of the launch.
-//   A CU works through its workgroups one round after another: `slots` of them fit the chip, and the last round counts whole
-//   (a row tile's CU with one of them alone takes 1.6 times as long for it as for half of two).  Cutting evens that
-//   out; each part costs the writing and reading of its sums.
-// Measured, one call's keys in 1, 2, 3, 4 parts: 444 tiles of 128 rows, 32 760 keys, d 128: 1031, 1027, 1017, 928 us (the
-// model: 4); 1056 of 64 rows, 4 400 keys, d 64: 162, 142, 133, 133 us (3).  One token, 131 000 keys, 12 key heads: 21 parts
-// 77, 42 (504 workgroups, 512 fit) 77, 43: 104, 85: 81, 170: 88 us; 128 heads of up to 8 000 keys: 2: 42, 4: 35, 8: 37, 16: 44 us.
+// How many parts the keys of a row are cut into: the number with the least time by a model of the launch.  Cutting
+// fills the chip and evens out its last round; each part costs the writing and reading of its sums.
+//
+// Tiles of many rows: a compute unit takes `fit` workgroups at once, k of them in fit / 3 + 2 k / 3 times one's time on a full
+// unit (few wavefronts leave it idle); more than that as they come, or, where the cache's bytes are the time, in rounds.
+// Measured (us, by parts): 43 tiles of 50 rows, 36 558 keys, d 128: 4: 251, 6: 200, 12: 140, 17: 112, 23: 103, 29: 121, 42: 114
+// (the model takes 23); 36 tiles of 128 rows, 32 760 keys, d 128: 4: 214, 8: 131, 12: 101, 21: 103, 32: 121 (21); 156 of them: 1:
+// 803, 3: 350, 5: 414, 8: 341, 12: 366 (8); 444: 1: 979, 2: 1014, 4: 910, 5: 933, 8: 954 (4); 16 tiles of 64 rows, 60 000 keys,
+// d 64: 12: 112, 23: 72, 42: 51, 64: 44, 85: 49, 128: 47 (128); 1056 of them, 4 400 keys: 1: 149, 2: 143, 3: 137, 5: 142 (3).
+// Few rows: the cache's bytes are all the time, and all workgroups should run at once.  One token, 131 000 keys, 12 key heads:
+// 21: 77, 42 (504 workgroups, 512 fit): 77, 43: 104, 85: 81, 170: 88; 128 heads of up to 8 000 keys: 2: 51, 4: 39, 8: 42, 16: 49.
 static int splits_of(const CacheAttnPlan &plan, const Problem &pb, int max_blocks, bool lists) {
-  const bool few = plan.tile_rows == 32;
+  constexpr int kUnits = 256;                          // compute units
+  const bool few = plan.tile_rows == 32, wide = pb.d == 128;
   const double keys = (double)max_blocks * pb.block * (lists ? 0.25 : 1.0);     // lists: what they may keep
-  const int64_t slots = few ? (pb.d == 128 ? 512 : 1024) : 256;
-  // one unit's time: the cache's bytes at its share of 5.5 TB/s, or its products at a CU's share of 1000 / 600 TFLOP/s
-  const double unit = few ? 2.0 * keys * pb.d / (5.5e12 / slots) : 4.0 * plan.tile_rows * keys * pb.d / ((pb.d == 128 ? 1.0e15 : 0.6e15) / 256);
+  const int fit = few ? (wide ? 2 : 4) : wide ? (plan.tile_rows == 64 ? 4 : 3) : (plan.tile_rows == 64 ? 8 : 4);   // registers, LDS
+  // a workgroup's time at its share of a full chip: its codes at 5.5 (tiles: 4.4) TB/s, or its products at 1000 / 600 TFLOP/s
+  const double copies = 2.0 * keys * pb.d / ((few ? 5.5e12 : 4.4e12) / kUnits);
+  const double products = 4.0 * plan.tile_rows * keys * pb.d / ((wide ? 1.0e15 : 0.6e15) / kUnits);
   const double part = 8.0 * plan.units * plan.rows_kept * pb.d / 8e12;
+  auto together = [&](int64_t k) { return k == 0 ? 0.0 : fit / 3.0 + 2.0 * k / 3.0; };
   int best = 1;
   double best_time = 1e30;
   for (int s = 1; s <= kMaxSplits && (s == 1 || (s * 256.0 <= keys && plan.units * s * plan.rows_kept * pb.d <= kMostSums)); ++s) {
-    const double rounds = (double)((plan.units * s + slots - 1) / slots);
-    const double time = (few || rounds > 1.0 ? rounds : 1.6) / s * unit + (few ? rounds * 2e-6 : 0.0) + (s > 1 ? s * part + 3e-6 : 0.0);
+    const int64_t n = (plan.units * s + kUnits - 1) / kUnits, full = n / fit * fit;
+    double time = s > 1 ? s * part + 3e-6 : 0.0;
+    if (few) time += (double)((plan.units * s + kUnits * fit - 1) / (kUnits * fit)) * (fit * copies / s + 2e-6);
+    else if (copies > products) time += ((double)full + together(n - full)) / s * copies;
+    else time += (n < fit ? together(n) : (double)n) / s * products;
     if (time < best_time) {
       best_time = time;
       best = s;
