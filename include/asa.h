@@ -347,7 +347,7 @@ int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *
  *   k  [B, H_kv, max_blocks, block/32, d/16, 32, 16]     token t of the group, channel 16 c + x at [c][t][x]
  *   v  [B, H_kv, max_blocks, block/32, d/32, 2, 32, 16]  token 8 m + 4 h + j, channel 32 c + x at
  *                                                        [c][h][x][4 m + j]  (m, j < 4; h < 2)
- *   k_scale, v_scale  [B, H_kv, max_blocks] fp32, positive
+ *   k_scale, v_scale  [B, H_kv, max_blocks] fp32, finite, >= 0
  * Token l of a sequence is token l % block of block l / block.  A sequence that begins behind positions
  * that were never written needs codes and scales there that mean something: code 0 and 2^-100, say.
  */
@@ -397,6 +397,7 @@ int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v,
  *          order; entries that are negative or at or past the sequence's last block are skipped.  Both
  *          NULL: every block.
  * o        [B, H, L, d] bf16 (o_stride); lse [B*H, L] fp32.  A row that sees nothing gets O = 0, LSE = -inf.
+ * A scale of V below 2^-100 counts as 2^-100; |V| beyond 2^96 may overflow the fp32 sums.
  * Codes are widened to bf16 (exact), products accumulate in fp32; probabilities, times the block's
  * scale of V, are rounded to bf16 before the second product.  What the cache holds at and past length[b]
  * has no influence, whatever the bytes are.  Runs of a call repeat bit for bit.

@@ -570,12 +570,19 @@ int asa_reorder_tokens(const asa_params *p, int32_t n_tensors, const void *const
 // ------------------------------------------------------------------ norm and rotation of queries and keys
 // The shape of a call that has only B, H, L, d (and block) of asa_params; strides are looked at apart.
 static int resolve_shape(const asa_params *p, int H, int block, Problem *pb) {
-  if (!p) return ASA_ERR_INVALID_ARG;
+  if (!p || p->B < 1 || H < 1) return ASA_ERR_INVALID_ARG;
   asa_params shape;
   memset(&shape, 0, sizeof(shape));
-  shape.B = p->B; shape.H = H; shape.L = p->L; shape.d = p->d;
+  shape.B = shape.H = 1; shape.L = p->L; shape.d = p->d;
   shape.block = block; shape.k_samples = 1; shape.tau = 0.5f; shape.r_max = 1.f;
-  return resolve(&shape, pb);
+  int rc = resolve(&shape, pb);
+  if (rc != ASA_OK) return rc;
+  // (the kernels of these calls take their work from one grid axis: many short sequences are ordinary here)
+  if ((int64_t)p->B * H >= (int64_t)1 << 31) return ASA_ERR_UNSUPPORTED;
+  pb->B = p->B;
+  pb->H = H;
+  pb->n_slabs = p->B * H;
+  return ASA_OK;
 }
 
 // The rows of a tensor that is written are apart from each other: along the axes in the order of their strides, each stride

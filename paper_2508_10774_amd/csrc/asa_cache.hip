@@ -343,6 +343,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // nearly all the weight the result carries that rounding, 2^-9, beside its own), and the sums' D multiplications are rare
 // instead of in nearly every step (4 680 queries on 32 760 keys, 12 heads of 128: 953 -> 925 us).
 constexpr float kSlack = 8.f;
+constexpr float kLeastScale = 7.8886091e-31f;     // 2^-100: probabilities down to 2^-26 times it are normal numbers
 constexpr float kLeastFactor = 1.17549435e-38f;   // (a factor of zero would make NaN of a masked score)
 
 // The two A operands that 16 codes of a tile are.
@@ -396,6 +397,7 @@ struct BlockScale {
   float inv_v;      // ... and their sum takes it off again
   __device__ __forceinline__ BlockScale(const CacheAttnArgs &a, float k, float v) {
     c = fmaxf(a.scale_log2 * k, kLeastFactor);
+    v = fmaxf(v, kLeastScale);
     log2_v = __builtin_amdgcn_logf(v);
     inv_v = __builtin_amdgcn_rcpf(v);     // (exact for a power of two, else within a last bit)
   }

@@ -184,6 +184,34 @@ def test_scales_of_any_size():
             _check(h, q, [256], _run(h, q, _i32([256]), (ptr, idx)), kept)
 
 
+def test_blocks_of_scale_zero_and_many_short_sequences():
+    """A block of zeros at a scale of 0 weighs in like any other; more (sequence, head) pairs than a grid axis holds."""
+    h = Held(16, 1, 1, 3, 64, 64, 192)
+    h.cache.k_scale[0, 0, 1] = 0.0
+    h.cache.v_scale[0, 0, 1] = 0.0
+    h.read()
+    for L in (1, 70):
+        q = _q(17, 1, 1, L, 64)
+        _check(h, q, [192], _run(h, q, _i32([192])))
+    B, H = 17000, 4
+    h = Held(18, B, 1, 1, 64, 64, 3)
+    q = _q(19, B, H, 1, 64)
+    o, lse = _run(h, q, torch.full((B,), 3, dtype=torch.int32, device="cuda"))
+    k, v = (torch.from_numpy(x).cuda()[:, :, :3] for x in (h.k, h.v))
+    s = torch.matmul(q.double(), k.transpose(-1, -2).contiguous()) / 8
+    want = torch.matmul(torch.softmax(s, -1), v)
+    # 2^-8 of the result and 2^-8 of sum p |v|, which is at most the largest |v|
+    allow = 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -12) * v.abs().amax(2, keepdim=True)
+    assert ((o.double() - want).abs() <= allow).all()
+    assert (lse.reshape(B, H, 1).double() - torch.logsumexp(s, -1)).abs().max() <= 1e-4
+    n = asa.QkNorm(H_kv=H)
+    p = asa.Params(B=B, H=H, L=1, d=64, block=64)
+    out = [torch.empty_like(q) for _ in range(2)]
+    asa.asa_qk_norm_rope(p, n, q, q, *out)
+    want = q.double() / (q.double().square().mean(-1, keepdim=True) + 1e-6).sqrt()
+    assert torch.equal(out[0], out[1]) and ((out[0].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18 * want.abs().amax(-1, keepdim=True)).all()
+
+
 def test_values_that_are_not_finite():
     """NaN among the keys a row sees makes that row NaN, and no row that does not see it."""
     h = Held(14, 1, 2, 4, 64, 64, 256)
