@@ -846,16 +846,37 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(const CacheAt
 #pragma unroll
     for (int g = 1; g < GROUPS; ++g) o += part[g][sub];
   } else {
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[first + (int64_t)s * a.rows_kept][0]);
-    for (int s = 0; s < a.splits; ++s) {
-      const int64_t at = first + (int64_t)s * a.rows_kept;
-      const f32x2 mine = ml[at];
-      if (mine[0] == -__builtin_inff() && mine[1] == 0.f) continue;
-      const float f = fast_exp2(mine[0] - m);
-      const f32x4 p = *reinterpret_cast<const f32x4 *>(a.partial + at * D + sub * 4);
-      l = __builtin_fmaf(mine[1], f, l);
+    // four parts at a time, their loads together
+    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+      f32x2 x[4];
+      f32x4 p[4];
+      bool counts[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(p[i], f, o[i]);
+      for (int e = 0; e < 4; ++e) {
+        const int64_t at = first + (int64_t)min(s0 + e, a.splits - 1) * a.rows_kept;
+        x[e] = ml[at];
+        p[e] = *reinterpret_cast<const f32x4 *>(a.partial + at * D + sub * 4);
+      }
+      float top = m;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        // (a part without a key has left its sums unwritten)
+        counts[e] = s0 + e < a.splits && !(x[e][0] == -__builtin_inff() && x[e][1] == 0.f);
+        if (counts[e]) top = fmaxf(top, x[e][0]);
+      }
+      const float kept = m == -__builtin_inff() && l == 0.f ? 0.f : fast_exp2(m - top);
+      m = top;
+      l *= kept;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] *= kept;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float f = fast_exp2(x[e][0] - top);
+        if (!counts[e]) continue;
+        l = __builtin_fmaf(x[e][1], f, l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(p[e][i], f, o[i]);
+      }
     }
   }
   int head, token;
