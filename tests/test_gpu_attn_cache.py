@@ -152,6 +152,27 @@ def test_one_token_on_long_sequences_is_split():
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
 
 
+@pytest.mark.parametrize("H,L,d,block,blocks,parts", [(12, 400, 64, 128, 40, (5, 64)), (12, 400, 128, 64, 70, (5, 64)),
+                                                      (18, 1500, 128, 128, 32, (2, 4)), (66, 1000, 64, 64, 30, (2, 4))])
+def test_many_rows_in_parts(H, L, d, block, blocks, parts):
+    """Thousands of rows whose keys are cut into a few parts, and into more than are joined at once; a sequence too short for
+    most of the parts; NaN in the workspace."""
+    h = Held(20, 2, H, blocks, d, block, blocks * block)
+    p = asa.Params(B=2, H=H, L=L, d=d, block=block)
+    rows = 2 * H * -(-L // block) * block
+    assert rows > 4096
+    cut = asa.asa_attn_cache_workspace_bytes(p, h.cache) // (rows * (d + 2) * 4)
+    assert parts[0] <= cut <= parts[1], cut
+    q = _q(21, 2, H, L, d, packed=True, gain=2.0)
+    length = [blocks * block - 3, 70]
+    o, lse = _run(h, q, _i32(length))
+    k, v = h.k, h.v
+    for head in (0, H // 2, H - 1):
+        one = slice(head, head + 1)
+        h.k, h.v = k[:, one], v[:, one]
+        _check(h, q[:, one], length, (o[:, one], lse.reshape(2, H, L)[:, one]))
+
+
 def test_strided_output_scale_and_canaries():
     h = Held(10, 2, 2, 3, 128, 64, 150)
     q = _q(11, 2, 4, 77, 128, packed=True)
@@ -182,6 +203,23 @@ def test_scales_of_any_size():
                 mask[..., lists] = True
                 ptr, idx, kept = _lists(mask)
             _check(h, q, [256], _run(h, q, _i32([256]), (ptr, idx)), kept)
+
+
+@pytest.mark.parametrize("span", [6.0, 40.0, 300.0])
+@pytest.mark.parametrize("falling", [False, True])
+def test_rising_and_falling_scores(span, falling):
+    """Scores that grow from key to key by little and by much (the running maximum is brought up late), or fall."""
+    h = Held(22, 1, 1, 6, 64, 64, 384)
+    ramp = torch.linspace(-1, 1, 384, device="cuda")
+    ramp = (ramp.flip(0) if falling else ramp)[None, None, :, None]
+    g = torch.Generator(device="cuda").manual_seed(23)
+    k = (ramp + 0.01 * torch.randn(1, 1, 384, 64, generator=g, device="cuda")).to(torch.bfloat16)
+    asa.asa_cache_write(asa.Params(B=1, H=1, L=384, d=64, block=64), h.cache, k, None)
+    h.read()
+    for L in (1, 40, 100):
+        q = torch.full((1, 1, L, 64), span / 8, device="cuda") * torch.linspace(0.2, 1, L, device="cuda")[:, None]
+        q = q.to(torch.bfloat16)
+        _check(h, q, [384], _run(h, q, _i32([384])))
 
 
 def test_blocks_of_scale_zero_and_many_short_sequences():
