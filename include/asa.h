@@ -400,7 +400,9 @@ int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v,
  * A scale of V below 2^-100 counts as 2^-100; |V| beyond 2^96 may overflow the fp32 sums.
  * Codes are widened to bf16 (exact), products accumulate in fp32; probabilities, times the block's
  * scale of V, are rounded to bf16 before the second product.  What the cache holds at and past length[b]
- * has no influence, whatever the bytes are.  Runs of a call repeat bit for bit.
+ * has no influence, whatever the bytes are.  Runs of a call repeat bit for bit; the last bits of o and lse may
+ * differ between calls of other sizes, of another max_blocks, or with lists instead of none (the keys of a row are
+ * added up in parts whose number depends on these).
  * L = 1 is a token-by-token step.  ceil(L/block) * max_blocks < 2^31.
  */
 size_t asa_attn_cache_workspace_bytes(const asa_params *p, const asa_kv_cache *c);
