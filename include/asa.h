@@ -392,10 +392,10 @@ int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v,
  * blocks its list keeps:
  *   S = scale * q K^T,  LSE = log sum exp S,  O = exp(S - LSE) V,   K, V = code value * scale.
  * length   DEVICE [B] int32, counts as clamped to [0, max_blocks * block]
- * row_ptr  [B*H_kv, ceil(L/block) + 1] int32, col_idx [B*H_kv, ceil(L/block) * max_blocks] int32: the
- *          lists of asa_build_mask, one for each block of queries and KEY head, of distinct blocks in any
- *          order; entries that are negative or at or past the sequence's last block are skipped.  Both
- *          NULL: every block.
+ * row_ptr  [B*H_kv, ceil(L/block) + 1] int32, col_idx [B*H_kv, ceil(L/block) * max_blocks] int32: lists as
+ *          asa_build_mask makes them (its own fit a cache of max_blocks = ceil(L/block)), one for each block of
+ *          queries and KEY head, of distinct blocks in any order; entries that are negative or at or past the
+ *          sequence's last block are skipped.  Both NULL: every block.
  * o        [B, H, L, d] bf16 (o_stride); lse [B*H, L] fp32.  A row that sees nothing gets O = 0, LSE = -inf.
  * A scale of V below 2^-100 counts as 2^-100; |V| beyond 2^96 may overflow the fp32 sums.
  * Codes are widened to bf16 (exact), products accumulate in fp32; probabilities, times the block's
