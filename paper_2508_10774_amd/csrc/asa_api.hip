@@ -74,8 +74,8 @@ int resolve(const asa_params *p, Problem *o) {
   if (p->block != 64 && p->block != 128) return ASA_ERR_UNSUPPORTED;
   memset(o, 0, sizeof(*o));
   o->B = p->B; o->H = p->H; o->L = p->L; o->d = p->d; o->block = p->block;
+  if (p->L > kMaxNb * p->block) return ASA_ERR_UNSUPPORTED;
   o->Nb = (p->L + p->block - 1) / p->block;
-  if (o->Nb > kMaxNb) return ASA_ERR_UNSUPPORTED;
   o->Lpad = o->Nb * p->block;
   o->n_slabs = p->B * p->H;
   // sampling (Alg. 2 steps 1-3): k offsets inside a block, shared by every block
@@ -578,7 +578,7 @@ static int resolve_shape(const asa_params *p, int H, int block, Problem *pb) {
   int rc = resolve(&shape, pb);
   if (rc != ASA_OK) return rc;
   // (the kernels of these calls take their work from one grid axis: many short sequences are ordinary here)
-  if ((int64_t)p->B * H >= (int64_t)1 << 31) return ASA_ERR_UNSUPPORTED;
+  if ((int64_t)p->B * H >= (int64_t)1 << 30) return ASA_ERR_UNSUPPORTED;
   pb->B = p->B;
   pb->H = H;
   pb->n_slabs = p->B * H;
@@ -592,11 +592,11 @@ static bool rows_apart(const TensorView &v, const Problem &pb) {
   for (int i = 0; i < 2; ++i)
     for (int j = 0; j < 2 - i; ++j)
       if (axis[j].stride > axis[j + 1].stride) std::swap(axis[j], axis[j + 1]);
-  int64_t inside = pb.d;
+  __int128 inside = pb.d;      // (strides are the caller's: any 64 bits)
   for (const auto &x : axis) {
     if (x.n == 1) continue;
     if (x.stride < inside) return false;
-    inside += (x.n - 1) * x.stride;
+    inside += (__int128)(x.n - 1) * x.stride;
   }
   return true;
 }

@@ -60,7 +60,7 @@ def test_norm_refusals():
                  dict(k=None, gk=None, dk=None), dict(qw=ctypes.c_void_p(0x10002)), dict(gq=odd), dict(dk=odd)):
         assert bwd(**args) == INVALID, args
     # rows that are written lie apart: a stride of 0, heads inside one another, tokens inside a head
-    for bad in ((0, 6400, 64), (25600, 0, 64), (25600, 64, 64), (25600, 6392, 64)):
+    for bad in ((0, 6400, 64), ((1 << 62) + 8, 1 << 62, 64), (25600, 0, 64), (25600, 64, 64), (25600, 6392, 64)):
         assert fwd(_params(), _norm(q_out_stride=bad)) == INVALID, bad
         assert L.asa_qk_norm_rope_bwd(_params(q_stride=bad), _norm(), *[FAKE] * 8, None, None, None, 0, None) == INVALID, bad
     need = ws(_params(), _norm())
