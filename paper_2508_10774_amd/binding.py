@@ -366,11 +366,15 @@ def asa_reorder_tokens(p: Params, src, dst, index, src_stride=None, dst_stride=N
 # norm and rotation of queries and keys; keys and values in 8 bits
 # ---------------------------------------------------------------------------
 
+# (the current device without the checks of torch.cuda around it: a device tensor is at hand when it is asked for)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _device(stream, first: torch.Tensor) -> int:
     """The device that the call's tensors have to be on: the current one, also for a stream of the caller's."""
     if not first.is_cuda:
         raise AsaError("libasa takes device tensors")
-    dev = torch.cuda.current_device()
+    dev = _current_device()
     if stream is not None and stream.device_index != dev:
         raise AsaError("the stream is not one of the current device")
     return dev
@@ -453,12 +457,13 @@ class QkNorm:
                 raise AsaError(f"cos, sin: [rows, {rot // 2}] expected, got {tuple(shape)} and {tuple(self.sin.shape)}")
             rows = shape[0]
             cos, sin = _flat(self.cos, "cos", f32, 0, dev), _flat(self.sin, "sin", f32, 0, dev)
+        start, qw, kw, qb, kb = self.start, self.q_weight, self.k_weight, self.q_bias, self.k_bias
         q_out, k_out = self.q_out_stride, self.k_out_stride
         return _packed(asa_qk_norm, _PACKED_NORM, (
             self.H_kv, _KINDS[self.kind], self.eps, rot, _PAIRINGS[self.pairing], rows, self.first_row,
-            _flat(self.start, "start", torch.int32, p.B, dev), cos, sin,
-            _flat(self.q_weight, "q_weight", f32, d, dev), _flat(self.k_weight, "k_weight", f32, d, dev),
-            _flat(self.q_bias, "q_bias", f32, d, dev), _flat(self.k_bias, "k_bias", f32, d, dev),
+            0 if start is None else _flat(start, "start", torch.int32, p.B, dev), cos, sin,
+            0 if qw is None else _flat(qw, "q_weight", f32, d, dev), 0 if kw is None else _flat(kw, "k_weight", f32, d, dev),
+            0 if qb is None else _flat(qb, "q_bias", f32, d, dev), 0 if kb is None else _flat(kb, "k_bias", f32, d, dev),
             q_out[0], q_out[1], q_out[2], k_out[0], k_out[1], k_out[2]))
 
 
