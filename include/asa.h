@@ -308,6 +308,7 @@ typedef struct asa_qk_norm {
   const float *q_bias, *k_bias;         /* DEVICE [d] fp32, ASA_NORM_LAYER only; NULL = zeros    */
   int64_t q_out_stride[3], k_out_stride[3];  /* of q_out / dq_out and k_out / dk_out, as in
                                 asa_params; all zero = packed [B, H, L, d], [B, H_kv, L, d]      */
+  int64_t dq_stride[3], dk_stride[3];        /* backward: of dq and dk; all zero = q_stride, k_stride */
 } asa_qk_norm;
 
 /*
@@ -324,11 +325,11 @@ int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, c
 /*
  * Its backward: from q, k (the forward's inputs; nothing else is kept) and the gradients dq_out,
  * dk_out of the outputs (q_out_stride, k_out_stride)
- *   dq, dk             bf16, q_stride and k_stride
+ *   dq, dk             bf16, dq_stride and dk_stride (the rows of q and k may then repeat)
  *   dq_weight, dk_weight, dq_bias, dk_bias  [d] fp32, sums over batch, heads and tokens; each may be NULL
  * Sums are formed in a fixed order: runs of a call repeat bit for bit.  dq may take the place of
  * q or of dq_out (the same strides), dk that of k or dk_out.  k = dk_out = dk = NULL: queries alone.
- * The biases' gradients belong to ASA_NORM_LAYER.
+ * The biases' gradients belong to ASA_NORM_LAYER.  The workspace depends on B, H, H_kv, L and d alone.
  */
 size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n);
 int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k,

@@ -44,6 +44,7 @@ class asa_qk_norm(ctypes.Structure):
         ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
         ("q_bias", ctypes.c_void_p), ("k_bias", ctypes.c_void_p),
         ("q_out_stride", ctypes.c_int64 * 3), ("k_out_stride", ctypes.c_int64 * 3),
+        ("dq_stride", ctypes.c_int64 * 3), ("dk_stride", ctypes.c_int64 * 3),
     ]
 
 
@@ -57,7 +58,7 @@ class asa_kv_cache(ctypes.Structure):
 # The same fields in one call (native sizes and alignment): setting them one by one takes 4 us, as long as a launch.
 _PACKED = struct.Struct("@6iP3fif12q")
 assert _PACKED.size == ctypes.sizeof(asa_params)
-_PACKED_NORM, _PACKED_CACHE = struct.Struct("@2if4i7P6q"), struct.Struct("@2i4P")
+_PACKED_NORM, _PACKED_CACHE = struct.Struct("@2if4i7P12q"), struct.Struct("@2i4P")
 assert _PACKED_NORM.size == ctypes.sizeof(asa_qk_norm) and _PACKED_CACHE.size == ctypes.sizeof(asa_kv_cache)
 
 EXPORTS = ["asa_version", "asa_error_string", "asa_last_hip_error", "asa_mask_workspace_bytes",
@@ -420,6 +421,16 @@ def _rows(t: Optional[torch.Tensor], what: str, shape, stride, dev: int) -> int:
     return t.data_ptr()
 
 
+def _own_strides(t: Optional[torch.Tensor], what: str, shape):
+    """Strides of batch, head and token that a tensor [B, heads, L, d] has itself (d where there is one: it says nothing); zeros for None."""
+    if t is None or t.dim() != 4:
+        return 0, 0, 0
+    d, got = shape[3], t.stride()
+    if got[3] != 1 or any(n > 1 and s < d for n, s in zip(shape[:3], got)):
+        raise AsaError(f"{what}: strides of rows that lie apart expected, got {got}")
+    return tuple(s if n > 1 else d for n, s in zip(shape[:3], got))
+
+
 _KINDS = {"rms": 0, "layer": 1}
 _PAIRINGS = {"adjacent": 0, "halves": 1}
 
@@ -446,7 +457,7 @@ class QkNorm:
     q_out_stride: Sequence[int] = (0, 0, 0)
     k_out_stride: Sequence[int] = (0, 0, 0)
 
-    def c(self, p: Params, dev: int) -> asa_qk_norm:
+    def c(self, p: Params, dev: int, dq_stride=(0, 0, 0), dk_stride=(0, 0, 0)) -> asa_qk_norm:
         if self.kind not in _KINDS or self.pairing not in _PAIRINGS:
             raise AsaError(f"kind {self.kind!r}: one of {list(_KINDS)}; pairing {self.pairing!r}: one of {list(_PAIRINGS)}")
         f32, d, rot = torch.float32, p.d, self.rot_dim
@@ -464,7 +475,7 @@ class QkNorm:
             0 if start is None else _flat(start, "start", torch.int32, p.B, dev), cos, sin,
             0 if qw is None else _flat(qw, "q_weight", f32, d, dev), 0 if kw is None else _flat(kw, "k_weight", f32, d, dev),
             0 if qb is None else _flat(qb, "q_bias", f32, d, dev), 0 if kb is None else _flat(kb, "k_bias", f32, d, dev),
-            q_out[0], q_out[1], q_out[2], k_out[0], k_out[1], k_out[2]))
+            q_out[0], q_out[1], q_out[2], k_out[0], k_out[1], k_out[2], *dq_stride, *dk_stride))
 
 
 def asa_qk_norm_rope(p: Params, n: QkNorm, q, k, q_out, k_out, stream=None):
@@ -477,20 +488,22 @@ def asa_qk_norm_rope(p: Params, n: QkNorm, q, k, q_out, k_out, stream=None):
 
 
 def asa_qk_norm_rope_bwd_workspace_bytes(p: Params, n: QkNorm) -> int:
-    """Depends on p's sizes and strides and on n.H_kv."""
+    """Depends on p's sizes and on n.H_kv."""
     c = asa_qk_norm(H_kv=n.H_kv)
     return int(load().asa_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(p.c()), ctypes.byref(c)))
 
 
 def asa_qk_norm_rope_bwd(p: Params, n: QkNorm, q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, dq_bias, dk_bias,
                          workspace, stream=None):
+    """The gradients of q and k, and of the parameters: dq and dk in the strides that they have themselves."""
     dev = _device(stream, q)
     qs, ks = (p.B, p.H, p.L, p.d), (p.B, n.H_kv or p.H, p.L, p.d)
     f32, d = torch.float32, p.d
+    dqs, dks = _own_strides(dq, "dq", qs), _own_strides(dk, "dk", ks)
     _check(load().asa_qk_norm_rope_bwd(
-        ctypes.byref(p.c()), ctypes.byref(n.c(p, dev)), _rows(q, "q", qs, p.q_stride, dev), _rows(k, "k", ks, p.k_stride, dev),
+        ctypes.byref(p.c()), ctypes.byref(n.c(p, dev, dqs, dks)), _rows(q, "q", qs, p.q_stride, dev), _rows(k, "k", ks, p.k_stride, dev),
         _rows(dq_out, "dq_out", qs, n.q_out_stride, dev), _rows(dk_out, "dk_out", ks, n.k_out_stride, dev),
-        _rows(dq, "dq", qs, p.q_stride, dev), _rows(dk, "dk", ks, p.k_stride, dev),
+        _rows(dq, "dq", qs, dqs, dev), _rows(dk, "dk", ks, dks, dev),
         _flat(dq_weight, "dq_weight", f32, d, dev), _flat(dk_weight, "dk_weight", f32, d, dev),
         _flat(dq_bias, "dq_bias", f32, d, dev), _flat(dk_bias, "dk_bias", f32, d, dev),
         _flat(workspace, "workspace", torch.uint8, 0, dev), workspace.nbytes if workspace is not None else 0,

@@ -601,7 +601,9 @@ static bool rows_apart(const TensorView &v, const Problem &pb) {
   return true;
 }
 
-static int check_norm(const asa_params *p, const asa_qk_norm *n, bool backward, NormArgs *a) {
+// What a call writes, whose rows have to lie apart: nothing yet (its sizes are asked for), the outputs, the gradients.
+enum class NormWrites { kNothing, kOutputs, kGradients };
+static int check_norm(const asa_params *p, const asa_qk_norm *n, NormWrites writes, NormArgs *a) {
   if (!p || !n) return ASA_ERR_INVALID_ARG;
   Problem q, k;
   int rc = resolve_shape(p, p->H, 128, &q);
@@ -624,8 +626,14 @@ static int check_norm(const asa_params *p, const asa_qk_norm *n, bool backward, 
   if (!view_from(p->q_stride, q, &a->side[0].in) || !view_from(n->q_out_stride, q, &a->side[0].out) ||
       !view_from(p->k_stride, k, &a->side[1].in) || !view_from(n->k_out_stride, k, &a->side[1].out))
     return ASA_ERR_INVALID_ARG;
-  if (!rows_apart(backward ? a->side[0].in : a->side[0].out, q) || !rows_apart(backward ? a->side[1].in : a->side[1].out, k))
-    return ASA_ERR_INVALID_ARG;
+  for (int i = 0; i < 2; ++i) {
+    NormSide &s = a->side[i];
+    const Problem &pb = i ? k : q;
+    const int64_t *st = i ? n->dk_stride : n->dq_stride;
+    s.dx = s.in;
+    if ((st[0] || st[1] || st[2]) && !view_from(st, pb, &s.dx)) return ASA_ERR_INVALID_ARG;
+    if (writes != NormWrites::kNothing && !rows_apart(writes == NormWrites::kGradients ? s.dx : s.out, pb)) return ASA_ERR_INVALID_ARG;
+  }
   a->side[0].heads = q.H; a->side[0].w = n->q_weight; a->side[0].b = n->q_bias;
   a->side[1].heads = k.H; a->side[1].w = n->k_weight; a->side[1].b = n->k_bias;
   a->start = n->start; a->cos_table = n->cos_table; a->sin_table = n->sin_table;
@@ -637,7 +645,7 @@ static int check_norm(const asa_params *p, const asa_qk_norm *n, bool backward, 
 int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k, void *q_out, void *k_out,
                      void *hip_stream) {
   NormArgs a;
-  int rc = check_norm(p, n, false, &a);
+  int rc = check_norm(p, n, NormWrites::kOutputs, &a);
   if (rc != ASA_OK) return rc;
   if (!q || !q_out || (k == nullptr) != (k_out == nullptr)) return ASA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return ASA_ERR_INVALID_ARG;
@@ -651,7 +659,7 @@ int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, c
 
 size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n) {
   NormArgs a;
-  if (check_norm(p, n, true, &a) != ASA_OK || plan_norm(&a, p->d) != ASA_OK) return 0;
+  if (check_norm(p, n, NormWrites::kNothing, &a) != ASA_OK || plan_norm(&a, p->d) != ASA_OK) return 0;
   return round256(norm_partial_bytes(a.side[0], p->d)) + round256(norm_partial_bytes(a.side[1], p->d));
 }
 
@@ -659,7 +667,7 @@ int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *
                          const void *dk_out, void *dq, void *dk, float *dq_weight, float *dk_weight, float *dq_bias,
                          float *dk_bias, void *workspace, size_t workspace_bytes, void *hip_stream) {
   NormArgs a;
-  int rc = check_norm(p, n, true, &a);
+  int rc = check_norm(p, n, NormWrites::kGradients, &a);
   if (rc != ASA_OK) return rc;
   if (!q || !dq_out || !dq || (k == nullptr) != (dk_out == nullptr) || (k == nullptr) != (dk == nullptr))
     return ASA_ERR_INVALID_ARG;

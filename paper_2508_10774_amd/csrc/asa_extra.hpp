@@ -11,7 +11,7 @@ struct NormSide {
   const void *src;        // x
   const void *grad;       // backward: gradient of the output
   void *dst;              // forward: the output; backward: dx
-  TensorView in, out;     // strides of x and dx; of the output and its gradient
+  TensorView in, out, dx; // strides of x; of the output and its gradient; of dx
   const float *w, *b;     // [d] or null
   float *partial;         // backward: [dweight, dbias][groups][d]
   float *dw, *db;         // [d] or null

@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(const NormAr
     const int t = there ? token : a.tokens - 1;
     const int b = t / a.L, l = t - b * a.L;
     const bf16 *src = reinterpret_cast<const bf16 *>(side.src) + b * side.in.sB + l * side.in.sL + sub * 8;
-    bf16 *dst = reinterpret_cast<bf16 *>(side.dst) + b * side.in.sB + l * side.in.sL + sub * 8;
+    bf16 *dst = reinterpret_cast<bf16 *>(side.dst) + b * side.dx.sB + l * side.dx.sL + sub * 8;
     const bf16 *grad = reinterpret_cast<const bf16 *>(side.grad) + b * side.out.sB + l * side.out.sL + sub * 8;
     u32x4 raw[kHeads], raw_g[kHeads];
 #pragma unroll
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_bwd_kernel(const NormAr
       sum = LAYER ? row_sum<LANES>(sum) * (1.0f / D) : 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = r * (dz[e] - __builtin_fmaf(x[e], along, sum));
-      if (there) *reinterpret_cast<u32x4 *>(dst + (int64_t)(head0 + i) * side.in.sH) = narrow8(x);
+      if (there) *reinterpret_cast<u32x4 *>(dst + (int64_t)(head0 + i) * side.dx.sH) = narrow8(x);
     }
   }
 
