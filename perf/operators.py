@@ -244,7 +244,7 @@ def prepare(case, seed):
         else:
             s["gq"], s["gk"] = (0.1 * torch.randn(B, n, L, d, device=DEV, generator=g) for n in (H, Hkv))
             s["gq"], s["gk"] = s["gq"].to(torch.bfloat16), s["gk"].to(torch.bfloat16)
-            s["dq"], s["dk"], _ = _heads(c["packed"], g, B, [H, Hkv, Hkv], L, d, 0.0)        # laid out as q and k
+            s.update(dq=_like(q), dk=_like(k))
             s["sums"] = {x: torch.zeros(d, device=DEV) for x in (("qw", "kw") if c["kind"] == "rms" else ("qw", "kw", "qb", "kb"))}
         return s
     Hkv, block = c["Hkv"], c["block"]
