@@ -403,7 +403,7 @@ int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v,
  * scale of V, are rounded to bf16 before the second product.  What the cache holds at and past length[b]
  * has no influence, whatever the bytes are.  Runs of a call repeat bit for bit; the last bits of o and lse may
  * differ between calls of other sizes, of another max_blocks, or with lists instead of none (the keys of a row are
- * added up in parts whose number depends on these).
+ * added up in parts whose number depends on these).  In calls of the same sizes they are the same whatever other rows hold.
  * L = 1 is a token-by-token step.  ceil(L/block) * max_blocks < 2^31.
  */
 size_t asa_attn_cache_workspace_bytes(const asa_params *p, const asa_kv_cache *c);

@@ -455,14 +455,16 @@ struct Rows {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
     const float m_new = fmaxf(m, max_of_halves(top) * bs.c);
-    if (__ballot(m_new - m > kSlack)) {
-      const float shrink = fast_exp2(m - m_new);
+    const bool grown = m_new - m > kSlack;
+    if (__ballot(grown)) {
+      // (each row by its own maximum alone, so that its bits are the same whatever the wavefront's other rows hold)
+      const float shrink = grown ? fast_exp2(m - m_new) : 1.f;
       l *= shrink;
 #pragma unroll
       for (int t = 0; t < T; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[t][i] *= shrink;
-      m = m_new;
+      m = grown ? m_new : m;
     }
     const float down = bs.log2_v - m;
     float sum = 0.f;
