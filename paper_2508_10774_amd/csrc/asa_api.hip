@@ -652,14 +652,14 @@ int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, c
   if (!k) a.side[1].heads = 0;
   a.side[0].src = q; a.side[0].dst = q_out;
   a.side[1].src = k; a.side[1].dst = k_out;
-  rc = plan_norm(&a, p->d);
+  rc = plan_norm(&a, p->d, false);
   if (rc != ASA_OK) return rc;
   return finish(launch_norm(a, p->d, n->kind == ASA_NORM_LAYER, n->pairing, false, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n) {
   NormArgs a;
-  if (check_norm(p, n, NormWrites::kNothing, &a) != ASA_OK || plan_norm(&a, p->d) != ASA_OK) return 0;
+  if (check_norm(p, n, NormWrites::kNothing, &a) != ASA_OK || plan_norm(&a, p->d, true) != ASA_OK) return 0;
   return round256(norm_partial_bytes(a.side[0], p->d)) + round256(norm_partial_bytes(a.side[1], p->d));
 }
 
@@ -677,7 +677,7 @@ int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *
       !aligned4(dq_weight) || !aligned4(dk_weight) || !aligned4(dq_bias) || !aligned4(dk_bias))
     return ASA_ERR_INVALID_ARG;
   if (!k) a.side[1].heads = 0;
-  rc = plan_norm(&a, p->d);
+  rc = plan_norm(&a, p->d, true);
   if (rc != ASA_OK) return rc;
   const size_t q_bytes = round256(norm_partial_bytes(a.side[0], p->d)), k_bytes = round256(norm_partial_bytes(a.side[1], p->d));
   if (!workspace || workspace_bytes < q_bytes + k_bytes || !aligned16(workspace)) return ASA_ERR_WORKSPACE;
@@ -718,8 +718,7 @@ static int cache_args(const asa_params *p, const asa_kv_cache *c, const void *k,
   // without `start` every sequence begins at a block's first token
   a->reached = start ? (pb.L + pb.block - 2) / pb.block + 1 : pb.Nb;
   if (a->reached > c->max_blocks) a->reached = c->max_blocks;
-  if ((int64_t)a->reached * a->H * a->B * a->n_sides >= ((int64_t)1 << 31)) return ASA_ERR_UNSUPPORTED;
-  return ASA_OK;
+  return plan_cache(*a, p->d, p->block);
 }
 
 int asa_cache_write(const asa_params *p, const asa_kv_cache *c, const void *k, const void *v, const int32_t *start,

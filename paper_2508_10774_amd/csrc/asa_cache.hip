@@ -337,7 +337,6 @@ __global__ __launch_bounds__((cache_threads<D, BLOCK>())) void cache_read_kernel
 namespace {
 
 constexpr int kMaxSplits = kThreads;
-constexpr int64_t kMostItems = ((int64_t)1 << 31) - 64;   // workgroups of a launch
 constexpr int64_t kMostSums = (int64_t)1 << 28;           // values of the parts' sums: 1 GB of workspace at most
 constexpr int64_t kFewRows = 4096;   // up to here the join has a workgroup for each row
 constexpr float kLn2 = 0.6931471805599453f;
@@ -945,7 +944,9 @@ int plan_cache_attn(const Problem &pb, int H_kv, int max_blocks, bool lists, Cac
   plan->rows_kept = (int)(rows < plan->tile_rows ? rows : plan->tile_rows);
   plan->units = (int64_t)pb.B * H_kv * pb.Nb * plan->tiles;
   plan->splits = 1;
-  if ((int64_t)pb.Nb * max_blocks >= ((int64_t)1 << 31) || plan->units >= kMostItems) return ASA_ERR_UNSUPPORTED;
+  if ((int64_t)pb.Nb * max_blocks >= ((int64_t)1 << 31)) return ASA_ERR_UNSUPPORTED;
+  // (keys are cut only where there are far fewer units than this: kMostSums)
+  if (!launch_fits((plan->units + kNumXcd - 1) / kNumXcd * kNumXcd, plan->tile_rows == 64 ? 128 : 256)) return ASA_ERR_UNSUPPORTED;
   plan->splits = splits_of(*plan, pb, max_blocks, lists);
   return ASA_OK;
 }
@@ -972,6 +973,12 @@ static hipError_t launch_cache_attn_as(const CacheAttnArgs &a, hipStream_t st) {
 hipError_t launch_cache_attn(const CacheAttnArgs &a, int D, hipStream_t st) {
   if (D == 128) return a.block == 128 ? launch_cache_attn_as<128, 128>(a, st) : launch_cache_attn_as<128, 64>(a, st);
   return a.block == 128 ? launch_cache_attn_as<64, 128>(a, st) : launch_cache_attn_as<64, 64>(a, st);
+}
+
+int plan_cache(const CacheArgs &a, int D, int block) {
+  const int64_t workgroups = (int64_t)a.reached * a.H * a.B * a.n_sides;
+  const int threads = block == 64 && D == 64 ? cache_threads<64, 64>() : kThreads;
+  return launch_fits(workgroups, threads) ? ASA_OK : ASA_ERR_UNSUPPORTED;
 }
 
 template <int D, int BLOCK>

@@ -6,6 +6,9 @@
 
 namespace asa {
 
+// Whether one launch holds the workgroups: HIP counts the threads along an axis in 32 bits.
+inline bool launch_fits(int64_t workgroups, int threads) { return workgroups * threads < (int64_t)1 << 32; }
+
 // Queries (side 0) or keys (side 1) of asa_qk_norm_rope and its backward.
 struct NormSide {
   const void *src;        // x
@@ -25,7 +28,7 @@ struct NormArgs {
   int rot, table_rows, first_row;
   float eps;
 };
-int plan_norm(NormArgs *a, int D);                          // fills in the work; asa_status
+int plan_norm(NormArgs *a, int D, bool backward);           // fills in the work; asa_status
 size_t norm_partial_bytes(const NormSide &s, int D);
 hipError_t launch_norm(const NormArgs &a, int D, bool layer, int pairing, bool backward, hipStream_t st);
 
@@ -44,6 +47,7 @@ struct CacheArgs {
   int B, H, L, max_blocks;
   int reached;            // blocks of a sequence that L tokens reach into, at most
 };
+int plan_cache(const CacheArgs &a, int D, int block);       // asa_status
 hipError_t launch_cache_write(const CacheArgs &a, int D, int block, hipStream_t st);
 hipError_t launch_cache_read(const CacheArgs &a, int D, int block, hipStream_t st);
 

@@ -303,7 +303,7 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(const NormArgs a, int D
 }
 
 // chunks, groups and tiles of a call; 0 = fits, else asa_status
-int plan_norm(NormArgs *a, int D) {
+int plan_norm(NormArgs *a, int D, bool backward) {
   const int64_t tokens = (int64_t)a->B * a->L;
   if (tokens >= ((int64_t)1 << 31) - 64) return ASA_ERR_UNSUPPORTED;
   const int per_tile = kThreads / (D / 8);
@@ -316,7 +316,10 @@ int plan_norm(NormArgs *a, int D) {
     const int64_t items = (int64_t)a->tiles * s.chunks;
     s.groups = (int)(items < kMaxGroups ? items : kMaxGroups);
   }
-  return chunks * a->tiles < ((int64_t)1 << 31) - 64 ? ASA_OK : ASA_ERR_UNSUPPORTED;
+  // (the backward's workgroups walk: their places, rounded up to whole shares, are counted in 31 bits)
+  const int64_t items = chunks * a->tiles, most = ((int64_t)1 << 31) - 2 * kMaxGroups;
+  const bool fits = backward ? items < most : launch_fits((items + kNumXcd - 1) / kNumXcd * kNumXcd, kThreads);
+  return fits ? ASA_OK : ASA_ERR_UNSUPPORTED;
 }
 
 size_t norm_partial_bytes(const NormSide &s, int D) { return (size_t)2 * s.groups * D * sizeof(float); }
