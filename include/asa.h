@@ -313,8 +313,8 @@ typedef struct asa_qk_norm {
 
 /*
  * q [B, H, L, d], k [B, H_kv, L, d] bf16 with p's q_stride and k_stride (slices of one projection
- * [B, L, heads * d], say) -> q_out, k_out bf16.  k = k_out = NULL: queries alone.  Of `p` only
- * B, H, L, d, q_stride and k_stride have a meaning.  L <= 131 072.  A tensor may be its own output
+ * [B, L, heads * d], say) -> q_out, k_out bf16.  k = k_out = NULL: queries alone
+ * (strides of keys then have no say).  Of `p` only B, H, L, d, q_stride and k_stride have a meaning.  L <= 131 072.  A tensor may be its own output
  * where the strides agree; any other overlap is undefined.  Here and in the calls below the rows of a
  * tensor that is written must lie apart (a stride of 0, for one: ASA_ERR_INVALID_ARG); tensors that are
  * only read may repeat rows.  A call whose launch would have 2^32 threads or more (256 for 16 tokens of 4 heads at d 128;
@@ -330,7 +330,8 @@ int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, c
  *   dq_weight, dk_weight, dq_bias, dk_bias  [d] fp32, sums over batch, heads and tokens; each may be NULL
  * Sums are formed in a fixed order: runs of a call repeat bit for bit.  dq may take the place of
  * q or of dq_out (the same strides), dk that of k or dk_out.  k = dk_out = dk = NULL: queries alone.
- * The biases' gradients belong to ASA_NORM_LAYER.  The workspace depends on B, H, H_kv, L and d alone.
+ * The biases' gradients belong to ASA_NORM_LAYER.  The workspace's size depends on B, H, H_kv, L and d
+ * alone (0 where a call with these strides would be refused).
  */
 size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n);
 int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k,

@@ -489,8 +489,8 @@ def asa_qk_norm_rope(p: Params, n: QkNorm, q, k, q_out, k_out, stream=None):
 
 def asa_qk_norm_rope_bwd_workspace_bytes(p: Params, n: QkNorm) -> int:
     """Depends on p's sizes and on n.H_kv."""
-    c = asa_qk_norm(H_kv=n.H_kv)
-    return int(load().asa_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(p.c()), ctypes.byref(c)))
+    s, c = asa_params(B=p.B, H=p.H, L=p.L, d=p.d), asa_qk_norm(H_kv=n.H_kv)
+    return int(load().asa_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(s), ctypes.byref(c)))
 
 
 def asa_qk_norm_rope_bwd(p: Params, n: QkNorm, q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, dq_bias, dk_bias,

@@ -603,7 +603,7 @@ static bool rows_apart(const TensorView &v, const Problem &pb) {
 
 // What a call writes, whose rows have to lie apart: nothing yet (its sizes are asked for), the outputs, the gradients.
 enum class NormWrites { kNothing, kOutputs, kGradients };
-static int check_norm(const asa_params *p, const asa_qk_norm *n, NormWrites writes, NormArgs *a) {
+static int check_norm(const asa_params *p, const asa_qk_norm *n, NormWrites writes, bool keys, NormArgs *a) {
   if (!p || !n) return ASA_ERR_INVALID_ARG;
   Problem q, k;
   int rc = resolve_shape(p, p->H, 128, &q);
@@ -623,13 +623,12 @@ static int check_norm(const asa_params *p, const asa_qk_norm *n, NormWrites writ
     return ASA_ERR_INVALID_ARG;
   if (n->kind == ASA_NORM_RMS && (n->q_bias || n->k_bias)) return ASA_ERR_INVALID_ARG;
   memset(a, 0, sizeof(*a));
-  if (!view_from(p->q_stride, q, &a->side[0].in) || !view_from(n->q_out_stride, q, &a->side[0].out) ||
-      !view_from(p->k_stride, k, &a->side[1].in) || !view_from(n->k_out_stride, k, &a->side[1].out))
-    return ASA_ERR_INVALID_ARG;
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < (keys ? 2 : 1); ++i) {      // (queries alone: the strides of keys have no say)
     NormSide &s = a->side[i];
     const Problem &pb = i ? k : q;
     const int64_t *st = i ? n->dk_stride : n->dq_stride;
+    if (!view_from(i ? p->k_stride : p->q_stride, pb, &s.in) || !view_from(i ? n->k_out_stride : n->q_out_stride, pb, &s.out))
+      return ASA_ERR_INVALID_ARG;
     s.dx = s.in;
     if ((st[0] || st[1] || st[2]) && !view_from(st, pb, &s.dx)) return ASA_ERR_INVALID_ARG;
     if (writes != NormWrites::kNothing && !rows_apart(writes == NormWrites::kGradients ? s.dx : s.out, pb)) return ASA_ERR_INVALID_ARG;
@@ -645,7 +644,7 @@ static int check_norm(const asa_params *p, const asa_qk_norm *n, NormWrites writ
 int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k, void *q_out, void *k_out,
                      void *hip_stream) {
   NormArgs a;
-  int rc = check_norm(p, n, NormWrites::kOutputs, &a);
+  int rc = check_norm(p, n, NormWrites::kOutputs, k != nullptr, &a);
   if (rc != ASA_OK) return rc;
   if (!q || !q_out || (k == nullptr) != (k_out == nullptr)) return ASA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return ASA_ERR_INVALID_ARG;
@@ -659,7 +658,7 @@ int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, c
 
 size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n) {
   NormArgs a;
-  if (check_norm(p, n, NormWrites::kNothing, &a) != ASA_OK || plan_norm(&a, p->d, true) != ASA_OK) return 0;
+  if (check_norm(p, n, NormWrites::kNothing, true, &a) != ASA_OK || plan_norm(&a, p->d, true) != ASA_OK) return 0;
   return round256(norm_partial_bytes(a.side[0], p->d)) + round256(norm_partial_bytes(a.side[1], p->d));
 }
 
@@ -667,7 +666,7 @@ int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *
                          const void *dk_out, void *dq, void *dk, float *dq_weight, float *dk_weight, float *dq_bias,
                          float *dk_bias, void *workspace, size_t workspace_bytes, void *hip_stream) {
   NormArgs a;
-  int rc = check_norm(p, n, NormWrites::kGradients, &a);
+  int rc = check_norm(p, n, NormWrites::kGradients, k != nullptr, &a);
   if (rc != ASA_OK) return rc;
   if (!q || !dq_out || !dq || (k == nullptr) != (dk_out == nullptr) || (k == nullptr) != (dk == nullptr))
     return ASA_ERR_INVALID_ARG;
@@ -709,7 +708,9 @@ static int cache_args(const asa_params *p, const asa_kv_cache *c, const void *k,
   if ((!k && !v) || !aligned16(k) || !aligned16(v) || !aligned4(start) || !aligned4(count)) return ASA_ERR_INVALID_ARG;
   memset(a, 0, sizeof(*a));
   TensorView kv, vv;
-  if (!view_from(p->k_stride, pb, &kv) || !view_from(p->v_stride, pb, &vv)) return ASA_ERR_INVALID_ARG;
+  memset(&kv, 0, sizeof(kv));
+  memset(&vv, 0, sizeof(vv));
+  if ((k && !view_from(p->k_stride, pb, &kv)) || (v && !view_from(p->v_stride, pb, &vv))) return ASA_ERR_INVALID_ARG;
   if (rows_written && ((k && !rows_apart(kv, pb)) || (v && !rows_apart(vv, pb)))) return ASA_ERR_INVALID_ARG;
   if (k) a->side[a->n_sides++] = CacheSide{c->k, c->k_scale, const_cast<void *>(k), kv, false};
   if (v) a->side[a->n_sides++] = CacheSide{c->v, c->v_scale, const_cast<void *>(v), vv, true};
