@@ -371,9 +371,9 @@ def asa_reorder_tokens(p: Params, src, dst, index, src_stride=None, dst_stride=N
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _device(stream, first: torch.Tensor) -> int:
+def _device(stream, first: Optional[torch.Tensor]) -> int:
     """The device that the call's tensors have to be on: the current one, also for a stream of the caller's."""
-    if not first.is_cuda:
+    if first is None or not first.is_cuda:
         raise AsaError("libasa takes device tensors")
     dev = _current_device()
     if stream is not None and stream.device_index != dev:
