@@ -288,7 +288,9 @@ int asa_reorder_tokens(const asa_params *p, int32_t n_tensors, const void *const
  *     ASA_ROPE_ADJACENT  a, b = channels 2 t, 2 t + 1
  *     ASA_ROPE_HALVES    a, b = channels t, t + rot_dim / 2
  * A row outside [0, table_rows) turns nothing (first_row = -n: n text tokens in front of the video).
- * Everything is fp32 until the one rounding of the result to bf16.
+ * Everything is fp32 until the one rounding of the result to bf16, the sums of squares too: a row whose largest |x| is beyond
+ * 2^60 or, with eps = 0, below 2^-50 is out of range.  A norm over the channels of all heads together (one weight of
+ * heads * d: Wan2.1's) is not one of these.
  */
 #define ASA_NORM_RMS 0
 #define ASA_NORM_LAYER 1
@@ -396,11 +398,13 @@ int asa_cache_read(const asa_params *p, const asa_kv_cache *c, void *k, void *v,
  *   S = scale * q K^T,  LSE = log sum exp S,  O = exp(S - LSE) V,   K, V = code value * scale.
  * length   DEVICE [B] int32, counts as clamped to [0, max_blocks * block]
  * row_ptr  [B*H_kv, ceil(L/block) + 1] int32, col_idx [B*H_kv, ceil(L/block) * max_blocks] int32: lists as
- *          asa_build_mask makes them (its own fit a cache of max_blocks = ceil(L/block)), one for each block of
- *          queries and KEY head, of distinct blocks in any order; entries that are negative or at or past the
- *          sequence's last block are skipped.  Both NULL: every block.
+ *          asa_build_mask makes them, one for each block of queries and KEY head, of distinct blocks in any order;
+ *          entries that are negative or at or past the sequence's last block are skipped.  Both NULL: every block.
+ *          asa_build_mask's own fit where L tokens are all that is held, max_blocks = ceil(L/block) and H_kv = H; for
+ *          a chunk on a longer cache, or shared key heads, the caller makes them.
  * o        [B, H, L, d] bf16 (o_stride); lse [B*H, L] fp32.  A row that sees nothing gets O = 0, LSE = -inf.
- * A scale of V below 2^-100 counts as 2^-100; |V| beyond 2^96 may overflow the fp32 sums.
+ * A scale of V below 2^-100 counts as 2^-100 (in a block of scale s keys of less than 2^-126 / s of the weight of the row's
+ * heaviest count as nothing: 2^-26 at 2^-100); |V| beyond 2^96 or |q| beyond 2^112 may overflow the fp32 sums.
  * Codes are widened to bf16 (exact), products accumulate in fp32; probabilities, times the block's
  * scale of V, are rounded to bf16 before the second product.  What the cache holds at and past length[b]
  * has no influence, whatever the bytes are.  Runs of a call repeat bit for bit; the last bits of o and lse may

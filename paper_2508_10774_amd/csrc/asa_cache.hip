@@ -738,7 +738,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(const Cach
 // Many rows: two or four wavefronts of 32 rows each walk the listed blocks together, 64 keys at a time; the codes of the
 // next 64 are copied to LDS meanwhile (two buffers), every wavefront widens what it reads.  Bound by the matrix and the
 // vector pipe, which overlap little (64 keys x 32 rows at D 128: 1024 cycles of products, 512 of widening, 540 of soft-max):
-// 4 680 queries on 32 760 tokens, 12 heads of 128: 877 us with the join = 1074 TFLOP/s; at D 64 the vector pipe alone decides.
+// 4 680 queries on 32 760 tokens, 12 heads of 128: 895 to 920 us with the join, from card to card = 1020 to 1050 TFLOP/s; at D 64
+// the vector pipe alone decides.
 template <int D, int BLOCK, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void cache_attn_tile_kernel(const CacheAttnArgs a) {
   constexpr int kKeys = 64, kBytes = kKeys * D, kCopies = kBytes / 1024 / WAVES;
@@ -906,9 +907,13 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(const CacheAt
 // Measured (us, by parts): 43 tiles of 50 rows, 36 558 keys, d 128: 4: 251, 6: 200, 12: 140, 17: 112, 23: 103, 29: 121, 42: 114
 // (the model takes 23); 36 tiles of 128 rows, 32 760 keys, d 128: 4: 214, 8: 131, 12: 101, 21: 103, 32: 121 (21); 156 of them: 1:
 // 803, 3: 350, 5: 414, 8: 341, 12: 366 (8); 444: 1: 979, 2: 1014, 4: 910, 5: 933, 8: 954 (4); 16 tiles of 64 rows, 60 000 keys,
-// d 64: 12: 112, 23: 72, 42: 51, 64: 44, 85: 49, 128: 47 (128); 1056 of them, 4 400 keys: 1: 149, 2: 143, 3: 137, 5: 142 (3).
+// d 64: 12: 112, 23: 72, 42: 51, 64: 44, 85: 49, 128: 47 (128); 1056 of them, 4 400 keys: 1: 149, 2: 143, 3: 137, 5: 142 (the
+// model has 3 and 5 within 0.2 us of each other and takes 5).
 // Few rows: the cache's bytes are all the time, and all workgroups should run at once.  One token, 131 000 keys, 12 key heads:
 // 21: 77, 42 (504 workgroups, 512 fit): 77, 43: 104, 85: 81, 170: 88; 128 heads of up to 8 000 keys: 2: 51, 4: 39, 8: 42, 16: 49.
+//
+// The lengths are on the device: the keys that are counted here, the 256 of a part among them, are those that the cache has room
+// for, or a quarter of them where there are lists.  A sequence that holds less is cut into as many parts, shorter or empty ones.
 static int splits_of(const CacheAttnPlan &plan, const Problem &pb, int max_blocks, bool lists) {
   constexpr int kUnits = 256;                          // compute units
   const bool few = plan.tile_rows == 32, wide = pb.d == 128;

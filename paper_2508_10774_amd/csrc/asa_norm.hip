@@ -6,7 +6,7 @@
 // is 2 (forward) or 3 (backward) bf16 values per channel from and to HBM and nothing else, so what
 // counts is that every wavefront has several loads in flight: a group of lanes takes one token and
 // kHeads heads of it, whose rows it loads before it works on the first; they share the token's angles.
-// At the Wan shape (32 760 tokens, 12 + 12 heads of 128): forward 79 us = 5.3 TB/s, a large copy's rate; backward
+// At 32 760 tokens, 12 + 12 heads of 128 out of one projection: forward 79 us = 5.3 TB/s, a large copy's rate; backward
 // 126 us = 4.9 TB/s and 4.7 us for the sums.  2 or 6 heads at once: 79, 82 us; with heads of 64 4 is best (95, 87, 88).
 #include "asa_common.hpp"
 #include "asa_extra.hpp"
