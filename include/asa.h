@@ -315,12 +315,13 @@ typedef struct asa_qk_norm {
 
 /*
  * q [B, H, L, d], k [B, H_kv, L, d] bf16 with p's q_stride and k_stride (slices of one projection
- * [B, L, heads * d], say) -> q_out, k_out bf16.  k = k_out = NULL: queries alone
- * (strides of keys then have no say).  Of `p` only B, H, L, d, q_stride and k_stride have a meaning.  L <= 131 072.  A tensor may be its own output
- * where the strides agree; any other overlap is undefined.  Here and in the calls below the rows of a
- * tensor that is written must lie apart (a stride of 0, for one: ASA_ERR_INVALID_ARG); tensors that are
- * only read may repeat rows.  A call whose launch would have 2^32 threads or more (256 for 16 tokens of 4 heads at d 128;
- * below, for a block of the cache or for 128 rows of queries) is ASA_ERR_UNSUPPORTED.
+ * [B, L, heads * d], say) -> q_out, k_out bf16.  k = k_out = NULL: queries alone (strides of keys then
+ * have no say).  Of `p` only B, H, L, d, q_stride and k_stride have a meaning.  L <= 131 072.  A tensor
+ * may be its own output where the strides agree; any other overlap is undefined.  Here and in the calls
+ * below the rows of a tensor that is written must lie apart (a stride of 0, for one:
+ * ASA_ERR_INVALID_ARG); tensors that are only read may repeat rows.  A call whose launch would have
+ * 2^32 threads or more (256 for 16 tokens of 4 heads at d 128; below, for a block of the cache or for
+ * 128 rows of queries) is ASA_ERR_UNSUPPORTED.
  */
 int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k,
                      void *q_out, void *k_out, void *hip_stream);
