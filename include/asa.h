@@ -334,7 +334,7 @@ int asa_qk_norm_rope(const asa_params *p, const asa_qk_norm *n, const void *q, c
  * Sums are formed in a fixed order: runs of a call repeat bit for bit.  dq may take the place of
  * q or of dq_out (the same strides), dk that of k or dk_out.  k = dk_out = dk = NULL: queries alone.
  * The biases' gradients belong to ASA_NORM_LAYER.  The workspace's size depends on B, H, H_kv, L and d
- * alone (0 where a call with these strides would be refused).
+ * alone (0 where the strides of q or k are none that a tensor may have).
  */
 size_t asa_qk_norm_rope_bwd_workspace_bytes(const asa_params *p, const asa_qk_norm *n);
 int asa_qk_norm_rope_bwd(const asa_params *p, const asa_qk_norm *n, const void *q, const void *k,
